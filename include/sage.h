@@ -360,6 +360,190 @@ int sage_attn_fwd_decode(const void *q, const int8_t *k_i8, const uint8_t *v_fp8
                          int B, int Hq, int Hkv, int Nq, int Nk, int d, int causal, float sm_scale, float p_r,
                          int split_keys, sage_dtype dt, void *stream, void *workspace, size_t workspace_bytes);
 
+/* ---- a paged K/V cache in 8 bits ---------------------------------------------------------------------------
+ *
+ * The calls above quantise whole sequences: the mean of K and the maxima of V are statistics of all tokens, so a cache of theirs cannot
+ * grow.  These keep a growing cache instead, for serving: tokens are appended, attended to, forked and freed, and every scale belongs to
+ * a block of SAGE_CACHE_BLOCK tokens of one head, for K as for V  [per-block scales as in Sec. 2.1].  The paper does not treat this path;
+ * Q and P~ stay in 16 bits here and all sums in binary32.
+ *
+ * Sequences live in SLOTS.  A slot has a length and a row of the page table, which names its pages in order; pages can be shared between
+ * slots and are counted.  Everything is device memory of the caller; the calls read lengths and tables on the device, so that a
+ * whole step can be captured in a HIP graph and replayed as sequences grow.  Values found there that make no sense (a page outside the
+ * pool, a length beyond the table's row) are never used as addresses: what depends on them reads as NaN, or is not written.
+ *
+ * A block of 64 tokens x d channels of one head is 64*d bytes, in the order in which a wavefront's lanes take the operands of their matrix
+ * instructions (every load of the attention kernel is 1 KB of neighbouring bytes, and nothing passes through LDS):
+ *   K  byte ((t * (d/64) + c) * 64 + 16*g + r) * 16 + e   is token 16*t + r, channel 64*c + 16*g + e    (t < 4, g < 4, r < 16, e < 16)
+ *   V  byte (c * 64 + 16*g + r) * 16 + 8*u + 4*h + i      is token 32*u + 16*h + 4*g + i, channel 16*c + r    (u < 2, h < 2, i < 4)
+ * and stands for code * scale.  With a = max|x| over the block's tokens (x = K - k_shift, or V), each step one binary32 operation:
+ *   SAGE_CACHE_I8    scale = a / 127, code = rne(x * (127 / a)), stored with 128 added
+ *   SAGE_CACHE_E4M3  scale = a / 448, code = e4m3_rne(x * (448 / a))
+ * Blocks with a < 2^-100 hold scale 0 and codes 0; blocks with an element that is not finite hold scale NaN and codes 0, so whoever attends
+ * to them sees NaN.  Tokens behind the last one of a sequence are zeros in its last block.
+ */
+#define SAGE_CACHE_BLOCK 64 /* tokens with one scale */
+#define SAGE_CACHE_TAIL 128 /* last tokens of a slot that are kept in 16 bits as well: token p at p % SAGE_CACHE_TAIL */
+#define SAGE_MAX_SLOTS 4096
+
+typedef enum { SAGE_CACHE_I8 = 0, SAGE_CACHE_E4M3 = 1 } sage_cache_format;
+
+/* Which pages belong to whom; shared by the caches of all layers. */
+typedef struct {
+    int32_t *table;  /* device, [slots][width]: page ids, -1 where there is none */
+    int32_t *lens;   /* device, [slots]: tokens of each slot, 0 if it is free    */
+    int32_t *refs;   /* device, [n_pages]: slots that name a page, 0 if it is free */
+    int slots;       /* 1 .. SAGE_MAX_SLOTS */
+    int width;       /* pages a slot can have, >= 1; width * page_tokens <= 2^22 */
+    int n_pages;     /* 1 .. 2^22 */
+    int page_tokens; /* a multiple of SAGE_CACHE_BLOCK, at most 65536 */
+} sage_page_table;
+
+/* The K/V cache of one layer.  All pointers are device pointers, 16-byte aligned. */
+typedef struct {
+    uint8_t *k, *v;           /* [n_pages][Hkv][page_tokens/64][64*d] codes */
+    float *k_scale, *v_scale; /* [n_pages][Hkv][page_tokens/64] */
+    void *k_tail, *v_tail;    /* [slots][Hkv][SAGE_CACHE_TAIL][d] of `dt`: K as appended (rotated, not shifted) and V */
+    const float *k_shift;     /* [Hkv][d], or NULL: a constant taken off K before it is quantised  [Sec. 3].  It moves all scores of a
+                                 row by the same number, so attention needs no correction. */
+    int Hkv, d;               /* d in {64, 128}; Hkv 1 .. 1024 */
+    sage_cache_format fmt;
+    sage_dtype dt;            /* of K, V, Q, the tails and the outputs */
+} sage_cache;
+
+/* The T rows of a call belong to B sequences: rows q_start[b] .. q_start[b+1]-1 (device int32 [B+1], ascending, within 0 .. T) to the
+ * b-th, or T/B rows each where q_start is NULL (T a multiple of B).  Rows that belong to none are neither read nor written.
+ * slots[b] (device int32 [B], or NULL for b itself) is the sequence's slot; a sequence whose slot is outside the table
+ * is padding: its rows are skipped too. */
+
+/* ---- rotary positions --------------------------------------------------- */
+
+/*
+ * Channels (i, i + rot/2) (SAGE_ROPE_HALF) or (2i, 2i + 1) (SAGE_ROPE_INTERLEAVED), i < rot/2, are a pair (a, b) that the position p turns by
+ * p * f_i:  (a cos - b sin, b cos + a sin) * magnitude; channels from rot on pass unchanged.  f_i = base^(-2i/rot), then by `scaling`:
+ *   SAGE_ROPE_PLAIN   as it is
+ *   SAGE_ROPE_LINEAR  f_i / factor
+ *   SAGE_ROPE_NTK     with base * factor^(rot/(rot-2)) for the base
+ *   SAGE_ROPE_YARN    f_i (1 - g) + f_i / factor * g, g rising from 0 to 1 over i between the pair that turns `high` times over
+ *                     trained_len tokens (rounded down) and the one that turns `low` times (rounded up); magnitude 0.1 ln(factor) + 1 if 0 is given
+ *   SAGE_ROPE_BANDS   f_i g + f_i / factor * (1 - g), g = (turns over trained_len - low) / (high - low) within 0 .. 1
+ * A plan holds f_i / (2 pi) in units of 2^-64 turns: position times frequency is then an exact product modulo one turn, so far
+ * positions lose nothing.
+ */
+typedef enum { SAGE_ROPE_HALF = 0, SAGE_ROPE_INTERLEAVED = 1 } sage_rope_layout;
+typedef enum { SAGE_ROPE_PLAIN = 0, SAGE_ROPE_LINEAR = 1, SAGE_ROPE_NTK = 2, SAGE_ROPE_YARN = 3, SAGE_ROPE_BANDS = 4 } sage_rope_scaling;
+typedef struct {
+    uint64_t turns[64]; /* rot/2 are used */
+    float magnitude;
+    int rot;            /* channels that turn: a multiple of 16, 16 .. 128 */
+    sage_rope_layout layout;
+} sage_rope_plan;
+
+/*
+ * Fill a plan (host call, no GPU work).  base > 1, factor > 0, magnitude > 0 or 0 for the scaling's own (1 but for
+ * SAGE_ROPE_YARN); trained_len >= 1 and 0 < low < high are read by SAGE_ROPE_YARN (customary: 1, 32) and SAGE_ROPE_BANDS (1, 4).
+ */
+int sage_rope_init(sage_rope_plan *plan, int rot, sage_rope_layout layout, sage_rope_scaling scaling, double base, double factor,
+                   int trained_len, double low, double high, double magnitude);
+
+/*
+ * Rotate Q and, in the same launch, K.
+ *   q, q_out   device, [T, Hq, d] of `dt` through strides                 (in, out)
+ *   k, k_out   device, [T, Hkv, d], both NULL (with Hkv = 0) for Q alone  (in, out)
+ *   positions  device, [T] int32, any sign                                (in)
+ *   *_strides  host, two ELEMENT strides {token, head}, NULL for contiguous [T, H, d]: multiples of 8, >= 0, <= 2^40; rows of an
+ *              output must not overlap.  In place (out == in with the same strides) is allowed; any other overlap is not.
+ *   transposed 0, or 1 for the transposed operator (the angles' signs turned): the gradient with respect to the input, and for
+ *              magnitude 1 the inverse
+ * d in {64, 128}, plan->rot <= d, 1 <= T <= 2^22, Hq + Hkv <= 4096.
+ */
+int sage_rope(const void *q, void *q_out, const void *k, void *k_out, const int32_t *positions, int T, int Hq, int Hkv, int d,
+              const int64_t *q_strides, const int64_t *q_out_strides, const int64_t *k_strides, const int64_t *k_out_strides,
+              const sage_rope_plan *plan, int transposed, sage_dtype dt, void *stream);
+
+/* ---- tokens into and out of the cache ----------------------------------- */
+
+/*
+ * Append T tokens.  The slots' lengths and pages already cover them (sage_pages_reserve): the last of sequence b's rows becomes
+ * token lens[slot] - 1.  Blocks that the tokens touch are written whole; the tokens that stood in a block begun before come
+ * from the slot's tail, so codes and scales do not depend on how many calls brought the tokens.  A sequence may be shortened (lower
+ * lens) to any length down to 64 tokens below the longest it has had, and goes on from there: drafted tokens are taken back so.  With
+ * `rope`, K is rotated by its index in the sequence, and rounded to `dt`, on the way.
+ *   k, v       device, [T, Hkv, d] of cache->dt through strides {token, head} as for sage_rope         (in)
+ * A slot may appear once in a call.  Pages that hold the touched blocks must not be shared (sage_pages_fork sees to that, unless a
+ * sequence is then shortened into a page that it shares).
+ * Rows in front of the sequence's start (more rows than lens) and blocks without a page are not written.
+ */
+int sage_paged_append(const sage_page_table *pages, const sage_cache *cache, const void *k, const void *v, const int64_t *k_strides,
+                      const int64_t *v_strides, const int32_t *q_start, const int32_t *slots, int B, int T, const sage_rope_plan *rope,
+                      void *stream);
+
+/*
+ * Read tokens back, in 16 bits: token i of sequence b becomes row k_start[b] + i of k_out and v_out, contiguous [total, Hkv, d] of
+ * cache->dt, for all rows of k_start (device int32 [B+1], ascending, within 0 .. total).  k_shift is added again.  Rows beyond a
+ * sequence's length are zeros.  (For prefixes that a call on contiguous K and V goes on with, and for moving a sequence elsewhere.)
+ */
+int sage_paged_gather(const sage_page_table *pages, const sage_cache *cache, void *k_out, void *v_out, const int32_t *k_start,
+                      const int32_t *slots, int B, int total, void *stream);
+
+/* ---- attention over the cache ------------------------------------------- */
+
+/*
+ * out[row] = softmax(sm_scale * Q K^T) V over the tokens of the row's sequence, for rows of any number per sequence: single tokens, drafts, chunks
+ * of prompts, mixed.
+ *   q, out      device, [T, Hq, d] of cache->dt through strides {token, head} as for sage_rope; Hq a multiple of Hkv  (in, out)
+ *   causal      1: the i-th of a sequence's n rows sees its first lens - n + i + 1 tokens (the rows are the last tokens of the
+ *               sequence); 0: all rows see all tokens.  A row that sees none is zeros.
+ *   max_len     the longest sequence the caller expects, 1 .. 2^22: sizes the launch.  Longer ones are right too, only slower.
+ *   split_keys  tokens per range: the keys of a sequence are cut into ranges that separate workgroups take, combined by a second
+ *               launch; a positive multiple of 64, or 0 for the library's choice, which sage_paged_split_keys reports.  A row's result
+ *               depends on its own sequence, T/B (which picks the row tile) and split_keys alone.
+ *   workspace   device, 256-byte aligned, >= sage_paged_workspace_bytes() (0 bytes: none needed, may be NULL); nothing in
+ *               it has to be initialised
+ *   sm_scale    as for the other attention calls
+ * Q K^T and P V run in 16-bit matrix instructions on the codes (exact in binary16; bfloat16 rows of Q are scaled by a power of two) with
+ * binary32 sums; P~ is rounded to binary16 after the block's V scale, relative to the largest so far, is multiplied in; maximum, sum
+ * and output are binary32.
+ */
+int sage_paged_split_keys(int T, int B, int Hq, int Hkv, int max_len);
+size_t sage_paged_workspace_bytes(int T, int B, int Hq, int Hkv, int d, int max_len, int split_keys);
+int sage_attn_fwd_paged(const void *q, void *out, const int64_t *q_strides, const int64_t *out_strides, const sage_page_table *pages,
+                        const sage_cache *cache, const int32_t *q_start, const int32_t *slots, int B, int T, int Hq, int max_len, int causal,
+                        float sm_scale, int split_keys, void *stream, void *workspace, size_t workspace_bytes);
+
+/* ---- pages --------------------------------------------------------------- */
+
+/*
+ * The upkeep of the page table, on the device and deterministic: free pages are given out lowest first, to the listed slots in
+ * their order.  Lists have 1 .. SAGE_MAX_SLOTS entries; entries that cannot be served are refused one by one: their status is -1, nothing of
+ * theirs changes; the others' is 0.  refs and table must agree when a call begins.
+ *
+ * sage_pages_reserve  n_new[i] more tokens (device int32, or NULL for 1 each) for slots[i]: lens grows, and the pages that this takes
+ *                     are entered.  Refused: a slot outside the table or listed before, n_new < 0, a row of the table or a pool without
+ *                     room (an entry that needs pages is served if all pages needed up to and with it are free).  Pages that a
+ *                     shortened sequence kept are used first.
+ * sage_pages_fork     slot dst[i] becomes a copy of slot src[i]: full pages are shared, a last page that is not full gets a copy of its
+ *                     own, which sage_pages_copy makes from page_moves[i] = {from, to} (-1, -1: none) and slot_moves[i] = {src, dst}
+ *                     (the tails; -1, -1 for a refused entry) in each layer's cache.  Refused: slots outside the table, a dst that is not
+ *                     empty, listed before or a src of this call, a pool without room.
+ * sage_pages_free     the slots' pages are given back (freed when no slot names them) and the slots are empty.  Slots outside the table and
+ *                     empty ones are passed over.
+ * sage_pages_compact  the live pages behind the first M (M: the number of live ones) move to the lowest free places, at most max_moves
+ *                     of them, the lowest first; table and refs follow.  moves[k] = {from, to}, -1 behind the last;
+ *                     counts = {M, moves}.  The caller then runs sage_pages_copy for each layer.
+ * sage_pages_copy     codes and scales of every page of page_moves to their new places and, with slot_moves, the tails.  Moves outside
+ *                     the pool are passed over; no page may be written twice or written and read in one call.
+ */
+int sage_pages_reserve(const sage_page_table *pages, const int32_t *slots, const int32_t *n_new, int n, int32_t *status, void *stream);
+int sage_pages_fork(const sage_page_table *pages, const int32_t *src, const int32_t *dst, int n, int32_t *status, int32_t *page_moves,
+                    int32_t *slot_moves, void *stream);
+int sage_pages_free(const sage_page_table *pages, const int32_t *slots, int n, void *stream);
+size_t sage_pages_compact_workspace_bytes(int n_pages);
+int sage_pages_compact(const sage_page_table *pages, int32_t *moves, int max_moves, int32_t *counts, void *stream, void *workspace,
+                       size_t workspace_bytes);
+int sage_pages_copy(const sage_page_table *pages, const sage_cache *cache, const int32_t *page_moves, int n_moves, const int32_t *slot_moves,
+                    int n_slot_moves, void *stream);
+
 /* ---- measurement aid -------------------------------------------------- */
 
 /*

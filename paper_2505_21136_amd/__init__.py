@@ -23,6 +23,9 @@ __all__ = [
     "v_fp8_to_token_major", "diag_mfma_rate", "diag_quant_kv_path", "decode_split_keys", "decode_workspace_bytes",
     "sage_attn_fwd_decode", "EXPORTS", "sage_quant_q4", "sage_quant_kv4", "sage_delta_s",
     "sage_attn_fwd_q4", "sage_attn_fwd_4bit", "workspace_bytes_4bit", "delta_s_to_key_order",
+    "rope_plan", "sage_rope", "PageTable", "PagedCache", "sage_paged_append", "sage_paged_gather", "paged_split_keys",
+    "paged_workspace_bytes", "sage_attn_fwd_paged", "sage_pages_reserve", "sage_pages_fork", "sage_pages_free",
+    "sage_pages_compact", "sage_pages_copy",
 ]
 
 SAGE_F16, SAGE_BF16 = 0, 1
@@ -33,7 +36,10 @@ EXPORTS = ["sage_get_params", "sage_strerror", "sage_v_fp8_bytes", "sage_quant_w
            "sage_quant_kv", "sage_quant_kv_static", "sage_diag_mfma_rate", "sage_diag_quant_kv_path", "sage_decode_split_keys", "sage_decode_workspace_bytes",
            "sage_attn_fwd_decode", "sage_delta_s_bytes",
            "sage_workspace_bytes_4bit", "sage_quant_q4", "sage_quant_kv4", "sage_delta_s", "sage_attn_fwd_q4",
-           "sage_attn_fwd_4bit"]
+           "sage_attn_fwd_4bit",
+           "sage_rope_init", "sage_rope", "sage_paged_append", "sage_paged_gather", "sage_paged_split_keys",
+           "sage_paged_workspace_bytes", "sage_attn_fwd_paged", "sage_pages_reserve", "sage_pages_fork", "sage_pages_free",
+           "sage_pages_compact_workspace_bytes", "sage_pages_compact", "sage_pages_copy"]
 
 
 class SageError(RuntimeError):
@@ -116,6 +122,7 @@ def lib() -> ctypes.CDLL:
         L.sage_attn_fwd_quantized.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, f, f, i, vp]
         L.sage_attn_fwd.restype = i
         L.sage_attn_fwd.argtypes = [vp, vp, vp, vp, i, i, i, i, i, f, vp, i, vp, sz]
+        _paged.declare(L)
         _lib = L
     return _lib
 
@@ -560,3 +567,9 @@ def v_fp8_to_token_major(v_fp8: torch.Tensor, N: int) -> torch.Tensor:
     x = v_fp8.reshape(B, H, T, d, 2, 4, 4, 4)       # [.., t>>2, g, t&3, i]
     x = x.permute(0, 1, 2, 4, 6, 5, 7, 3)           # [B, H, T, t>>2, t&3, g, i, d]
     return x.reshape(B, H, T * 128, d)[:, :, :N].contiguous()
+
+
+from . import paged as _paged  # noqa: E402  (the paged cache uses the helpers above)
+from .paged import (PagedCache, PageTable, paged_split_keys, paged_workspace_bytes, rope_plan, sage_attn_fwd_paged,  # noqa: E402
+                    sage_paged_append, sage_paged_gather, sage_pages_compact, sage_pages_copy, sage_pages_fork,
+                    sage_pages_free, sage_pages_reserve, sage_rope)

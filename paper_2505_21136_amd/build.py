@@ -22,7 +22,12 @@ UNITS = [
     ("sage_prefill.hip", []),
     ("sage_spread.hip", []),
     ("sage_decode.hip", []),
+    ("sage_rope.hip", ["-ffp-contract=off"]),
+    ("sage_paged.hip", ["-ffp-contract=off"]),
+    ("sage_paged_attn.hip", []),
+    ("sage_pages.hip", []),
     ("sage_api.hip", []),
+    ("sage_api_paged.hip", []),
     ("sage_diag.hip", []),
 ]
 
@@ -32,6 +37,7 @@ def sources():
     out.append(os.path.join(CSRC, "sage_internal.h"))
     out.append(os.path.join(CSRC, "sage_attn_device.h"))
     out.append(os.path.join(CSRC, "sage_tile_copy.h"))
+    out.append(os.path.join(CSRC, "sage_paged.h"))
     out.append(os.path.join(os.path.dirname(HERE), "include", "sage.h"))
     return out
 

@@ -6,6 +6,7 @@
 // speaks of this call's own launches.
 #include "../../include/sage.h"
 #include "sage_internal.h"
+#include "sage_paged.h"
 
 #include <math.h>
 
@@ -151,6 +152,8 @@ Fwd4Workspace fwd4_layout(void *base, int B, int Hq, int Hkv, int Nq, int Nk, in
 
 }  // namespace
 
+int sage::status_of(hipError_t e) { return from_hip(e); }
+
 extern "C" {
 
 int sage_get_params(sage_params *out) {
@@ -169,7 +172,7 @@ const char *sage_strerror(int code) {
         case SAGE_OK: return "success";
         case SAGE_EINVAL:
             return "invalid argument (NULL or misaligned pointer, d not 64/128, size out of range, bad dtype or FP8 "
-                   "range, Hq not a multiple of Hkv, causal with Nk < Nq)";
+                   "range, Hq not a multiple of Hkv, causal with Nk < Nq, bad strides or page geometry)";
         case SAGE_EWORKSPACE: return "workspace missing, misaligned or too small";
         case SAGE_EHIP: return hipGetErrorString(g_last_hip_error);
         case SAGE_ESCRATCH:

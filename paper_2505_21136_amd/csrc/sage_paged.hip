@@ -1,0 +1,383 @@
+// Tokens into and out of the paged 8-bit cache, and copies of its pages (gfx950).  Memory-bound: each kernel reads what it needs once
+// and writes it once, in runs of 16 bytes a lane where the layout allows.
+//
+// The unit compiles without contraction: the quantiser's steps are defined one binary32 operation each.
+#include "sage_paged.h"
+
+#include <float.h>
+
+#include <algorithm>
+
+namespace sage {
+namespace {
+
+constexpr int kBlock = SAGE_CACHE_BLOCK, kTail = SAGE_CACHE_TAIL;
+constexpr float kTiny = 0x1p-100f;
+
+// Codes of eight values, one per byte.
+template <bool E4M3>
+__device__ __forceinline__ uint2 cache_codes(const float (&x)[8], float factor) {
+    if constexpr (!E4M3) {
+        const uint2 w = int8_codes(x, factor);
+        return make_uint2(w.x ^ 0x80808080u, w.y ^ 0x80808080u);  // + 128
+    } else {
+        int w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * factor, x[4 * i + 1] * factor, 0, false);
+            w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * factor, x[4 * i + 3] * factor, w[i], true);
+        }
+        return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+    }
+}
+
+// A block's scale and the factor on its values from its largest one; `bad`: an element is not finite (scale NaN, and the values that the
+// caller passes on are to be zeros).
+template <bool E4M3>
+__device__ __forceinline__ void block_scale(float a, bool bad, float &scale, float &factor) {
+    constexpr float R = E4M3 ? 448.0f : 127.0f;
+    const bool some = !bad && a >= kTiny;
+    scale = bad ? __builtin_nanf("") : some ? a / R : 0.0f;
+    factor = some ? R / a : 0.0f;
+}
+
+struct AppendArgs {
+    sage_page_table pt;
+    sage_cache c;
+    const uint16_t *k, *v;
+    TokenStrides k_st, v_st;
+    Batch bt;
+    int rope;
+};
+
+// One workgroup of 2 D threads quantises one block of 64 tokens of one head, of K (blockIdx.y even) or V, whatever part of it is new: tokens
+// of earlier calls come from the slot's tail.
+//   K: a thread takes 16 channels of two tokens (the 8 pairs that rotate together), which are 16 neighbouring bytes of the cache,
+//      or two runs of 8.
+//   V: a thread takes 2 channels of the 16 tokens whose codes are neighbours in the cache, 16 bytes per channel; a wavefront's loads are
+//      whole rows of 256 bytes.
+// The tail's two halves hold the tokens of the sequence's last two blocks.  The half that the first touched block stands in is
+// written by that block's workgroup alone, after it has read it (a barrier in between); the other half by the next block's.  So no
+// workgroup writes what another reads.
+template <int D, bool BF16, bool E4M3>
+__global__ __launch_bounds__(2 * D) void append_kernel(const AppendArgs a, const sage_rope_plan plan) {
+    __shared__ int found[2];
+    __shared__ float red[2][4];
+    constexpr int WAVES = 2 * D / 64;
+    const int Hkv = a.c.Hkv, h = (int)(blockIdx.y >> 1);
+    const bool is_v = blockIdx.y & 1;
+    int b, x;
+    if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 2, b, x, found)) return;
+    int q0, n;
+    rows_of(a.bt, b, q0, n);
+    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    if (n == 0 || slot < 0 || slot >= a.pt.slots) return;
+    const int len = min(a.pt.lens[slot], a.pt.width * a.pt.page_tokens);
+    const int start = max(len - n, 0);  // first new token; row q0 + p - (len - n) is token p
+    const int row0 = q0 - (len - n);
+    const int j0 = start / kBlock, jl = (len - 1) / kBlock, j = j0 + x;
+    if (len <= 0 || j > jl) return;
+    const uint16_t *src = is_v ? a.v : a.k;
+    const TokenStrides st = is_v ? a.v_st : a.k_st;
+    uint16_t *tail = static_cast<uint16_t *>(is_v ? a.c.v_tail : a.c.k_tail) + ((size_t)slot * Hkv + h) * kTail * D;
+    const uint16_t *head = src + h * st.h;
+    const int tid = threadIdx.x;
+    // the block whose tokens this workgroup puts into the tail: the last or the last but one, of its parity
+    const int keep = (x == 0 || x == 1) ? ((jl ^ j) & 1 ? jl - 1 : jl) : -1;
+
+    // K's values, 8 pairs (or 16 channels) of token p of the block jj, rotated and rounded, as 16-bit values
+    const int item = tid % (D / 16), half = plan.rot / 2;
+    const bool turns = a.rope && 16 * item < plan.rot, halves = turns && plan.layout == SAGE_ROPE_HALF;
+    const int c0 = halves ? 8 * item : 16 * item, c1 = halves ? half + 8 * item : 16 * item + 8;
+    const auto load_k = [&](int p, uint4 (&w)[2]) {
+        w[0] = w[1] = make_uint4(0, 0, 0, 0);
+        if (p >= len) return;
+        const bool fresh = p >= start;
+        const uint16_t *r = fresh ? head + (int64_t)(row0 + p) * st.t : tail + (size_t)(p % kTail) * D;
+        w[0] = *reinterpret_cast<const uint4 *>(r + c0);
+        w[1] = *reinterpret_cast<const uint4 *>(r + c1);
+        if (fresh && turns) {
+            float cs[8], sn[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                rope_angle(p, plan.turns[8 * item + i], cs[i], sn[i]);
+                cs[i] *= plan.magnitude;
+                sn[i] *= plan.magnitude;
+            }
+            rope_turn<BF16>(halves, cs, sn, w[0], w[1]);
+        }
+    };
+    // V's: channels 2 cp, 2 cp + 1 of the block's tokens 32 u + 16 hh + 4 g + i, one 32-bit word a token
+    const int g = tid / (D / 2), cp = tid % (D / 2);
+    const auto v_token = [&](int i) { return 32 * (i >> 3) + 16 * (i >> 2 & 1) + 4 * g + (i & 3); };
+    const auto load_v = [&](int p) -> uint32_t {
+        if (p >= len) return 0;
+        const uint16_t *r = p >= start ? head + (int64_t)(row0 + p) * st.t : tail + (size_t)(p % kTail) * D;
+        return *reinterpret_cast<const uint32_t *>(r + 2 * cp);
+    };
+    const int p0 = j * kBlock, r0 = tid / (D / 16);
+
+    // ---- the block's values, its largest one, and whether all are finite ----
+    float f[4][8];  // K: token r0 (two runs of 8), token r0 + 32 (two); V: [channel][token] in two halves of 8
+    uint4 kw[2][2];
+    uint32_t vw[16];
+    if (!is_v) {
+        float sh[2][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sh[0][i] = a.c.k_shift ? a.c.k_shift[h * D + c0 + i] : 0.0f;
+            sh[1][i] = a.c.k_shift ? a.c.k_shift[h * D + c1 + i] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int p = p0 + r0 + 32 * e;
+            load_k(p, kw[e]);
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                unpack8<BF16>(kw[e][o], f[2 * e + o]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[2 * e + o][i] = p < len ? f[2 * e + o][i] - sh[o][i] : 0.0f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) vw[i] = load_v(p0 + v_token(i));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            f[i >> 3][i & 7] = to_f32<BF16>(vw[i] & 0xffffu);
+            f[2 + (i >> 3)][i & 7] = to_f32<BF16>(vw[i] >> 16);
+        }
+    }
+    float amax = 0.0f, odd = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            amax = fmaxf(amax, fabsf(f[e][i]));
+            if (!(fabsf(f[e][i]) <= FLT_MAX)) odd = 1.0f;
+        }
+    amax = wave_max(amax);
+    odd = wave_max(odd);
+    if ((tid & 63) == 0) red[0][tid >> 6] = amax, red[1][tid >> 6] = odd;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) amax = fmaxf(amax, red[0][w]), odd = fmaxf(odd, red[1][w]);
+    const bool bad = odd != 0.0f;
+    float scale, factor;
+    block_scale<E4M3>(amax, bad, scale, factor);
+    if (bad) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[e][i] = 0.0f;
+    }
+
+    // ---- codes and scale ----
+    int in_page;
+    const int per_page = a.pt.page_tokens / kBlock, page = page_of(a.pt, slot, j, per_page, in_page);
+    if (page >= 0) {
+        const size_t blk = ((size_t)page * Hkv + h) * per_page + in_page;
+        uint8_t *out = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
+        if (tid == 0) (is_v ? a.c.v_scale : a.c.k_scale)[blk] = scale;
+        if (!is_v) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = r0 + 32 * e;
+                const uint2 lo = cache_codes<E4M3>(f[2 * e], factor), hi = cache_codes<E4M3>(f[2 * e + 1], factor);
+                const auto at = [&](int ch) { return (((r >> 4) * (D / 64) + (ch >> 6)) * 64 + (ch >> 4 & 3) * 16 + (r & 15)) * 16 + (ch & 15); };
+                *reinterpret_cast<uint2 *>(out + at(c0)) = lo;
+                *reinterpret_cast<uint2 *>(out + at(c1)) = hi;
+            }
+        } else {
+#pragma unroll
+            for (int ch = 0; ch < 2; ++ch) {
+                const uint2 lo = cache_codes<E4M3>(f[2 * ch], factor), hi = cache_codes<E4M3>(f[2 * ch + 1], factor);
+                const int c = 2 * cp + ch;
+                *reinterpret_cast<uint4 *>(out + ((c >> 4) * 64 + 16 * g + (c & 15)) * 16) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+        }
+    }
+
+    // ---- the tail ----
+    if (keep < j) return;
+    const int k0 = keep * kBlock;
+    if (!is_v) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int p = k0 + r0 + 32 * e;
+            if (p < start || p >= len) continue;
+            if (keep != j) load_k(p, kw[e]);
+            *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c0) = kw[e][0];
+            *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c1) = kw[e][1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int p = k0 + v_token(i);
+            if (p < start || p >= len) continue;
+            if (keep != j) vw[i] = load_v(p);
+            *reinterpret_cast<uint32_t *>(tail + (size_t)(p % kTail) * D + 2 * cp) = vw[i];
+        }
+    }
+}
+
+struct GatherArgs {
+    sage_page_table pt;
+    sage_cache c;
+    uint16_t *k, *v;
+    Batch bt;
+};
+
+// One workgroup of 2 D threads reads one block of one head back, of K or V; threads as in append_kernel, but for K, where neighbouring
+// lanes take neighbouring channels of a token: the rows that are written are twice the bytes of the codes that are read.
+template <int D, bool BF16, bool E4M3>
+__global__ __launch_bounds__(2 * D) void gather_kernel(const GatherArgs a) {
+    __shared__ int found[2];
+    const int Hkv = a.c.Hkv, h = (int)(blockIdx.y >> 1), tid = threadIdx.x;
+    const bool is_v = blockIdx.y & 1;
+    int b, j;
+    if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 1, b, j, found)) return;
+    int q0, n;
+    rows_of(a.bt, b, q0, n);
+    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    const int rows = min(n - j * kBlock, kBlock);  // rows of this block that the caller wants
+    if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
+    const int per_page = a.pt.page_tokens / kBlock;
+    const int there = min(max(a.pt.lens[slot], 0) - j * kBlock, kBlock);  // tokens of it that the sequence has
+    const bool beyond = (int64_t)j * kBlock >= (int64_t)a.pt.width * a.pt.page_tokens;
+    int in_page;
+    const int page = beyond ? -1 : page_of(a.pt, slot, j, per_page, in_page);
+    const size_t blk = page < 0 ? 0 : ((size_t)page * Hkv + h) * per_page + in_page;
+    const uint8_t *codes = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
+    const float scale = page < 0 ? __builtin_nanf("") : (is_v ? a.c.v_scale : a.c.k_scale)[blk];
+    uint16_t *out = (is_v ? a.v : a.k) + ((int64_t)(q0 + j * kBlock) * Hkv + h) * D;
+    const int64_t st = (int64_t)Hkv * D;
+    const auto value = [&](uint32_t w, int i) -> float {
+        const uint32_t c = w >> (8 * i) & 0xffu;
+        float x;
+        if constexpr (E4M3) x = __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+        else x = (float)((int)c - 128);
+        return x * scale;
+    };
+    if (!is_v) {
+        const int item = tid % (D / 16);
+        float sh[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sh[i] = a.c.k_shift ? a.c.k_shift[h * D + 16 * item + i] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = tid / (D / 16) + 32 * e;
+            if (r >= rows) continue;
+            const uint4 w = *reinterpret_cast<const uint4 *>(codes + (((r >> 4) * (D / 64) + (item >> 2)) * 64 + (item & 3) * 16 + (r & 15)) * 16);
+            const uint32_t c[4] = {w.x, w.y, w.z, w.w};
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float u = value(c[i >> 1], 2 * (i & 1)) + sh[2 * i], v = value(c[i >> 1], 2 * (i & 1) + 1) + sh[2 * i + 1];
+                y[i] = r < there ? pack2<BF16>(u, v) : 0;
+            }
+            uint4 *o = reinterpret_cast<uint4 *>(out + r * st + 16 * item);
+            o[0] = make_uint4(y[0], y[1], y[2], y[3]);
+            o[1] = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+    } else {
+        const int g = tid / (D / 2), cp = tid % (D / 2), c = 2 * cp;
+        const uint4 lo = *reinterpret_cast<const uint4 *>(codes + ((c >> 4) * 64 + 16 * g + (c & 15)) * 16);
+        const uint4 hi = *reinterpret_cast<const uint4 *>(codes + ((c >> 4) * 64 + 16 * g + (c & 15) + 1) * 16);
+        const uint32_t u[4] = {lo.x, lo.y, lo.z, lo.w}, v[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 32 * (i >> 3) + 16 * (i >> 2 & 1) + 4 * g + (i & 3);
+            if (r >= rows) continue;
+            const uint32_t y = r < there ? pack2<BF16>(value(u[i >> 2], i & 3), value(v[i >> 2], i & 3)) : 0;
+            *reinterpret_cast<uint32_t *>(out + r * st + c) = y;
+        }
+    }
+}
+
+struct CopyArgs {
+    uint8_t *base[4];      // k, v, k_scale, v_scale
+    int64_t bytes[4];      // of a page
+    uint8_t *tail[2];
+    int64_t tail_bytes;    // of a slot
+    const int32_t *page_moves, *slot_moves;
+    int n_moves, n_pages, slots, chunks;
+};
+
+// `chunks` workgroups share a move's bytes, 16 (scales: 4) at a time.
+__global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
+    const int move = (int)blockIdx.x / a.chunks, chunk = (int)blockIdx.x % a.chunks;
+    const bool pages = move < a.n_moves;
+    const int32_t *m = pages ? a.page_moves + 2 * (size_t)move : a.slot_moves + 2 * ((size_t)move - a.n_moves);
+    const int from = m[0], to = m[1], end = pages ? a.n_pages : a.slots;
+    if (from < 0 || to < 0 || from >= end || to >= end || from == to) return;
+    const int64_t first = (int64_t)chunk * blockDim.x + threadIdx.x, step = (int64_t)a.chunks * blockDim.x;
+    const auto copy16 = [&](uint8_t *p, int64_t bytes) {
+        const uint4 *s = reinterpret_cast<const uint4 *>(p + from * bytes);
+        uint4 *d = reinterpret_cast<uint4 *>(p + to * bytes);
+        for (int64_t i = first; i < bytes / 16; i += step) d[i] = s[i];
+    };
+    if (!pages) {
+        copy16(a.tail[0], a.tail_bytes);
+        copy16(a.tail[1], a.tail_bytes);
+        return;
+    }
+    copy16(a.base[0], a.bytes[0]);
+    copy16(a.base[1], a.bytes[1]);
+#pragma unroll
+    for (int k = 2; k < 4; ++k) {
+        const uint32_t *s = reinterpret_cast<const uint32_t *>(a.base[k] + from * a.bytes[k]);
+        uint32_t *d = reinterpret_cast<uint32_t *>(a.base[k] + to * a.bytes[k]);
+        for (int64_t i = first; i < a.bytes[k] / 4; i += step) d[i] = s[i];
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const sage_page_table &pt, const sage_cache &c, const void *k, TokenStrides k_st, const void *v,
+                               TokenStrides v_st, const Batch &bt, const sage_rope_plan *rope, hipStream_t stream) {
+    AppendArgs a{pt, c, static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), k_st, v_st, bt, rope != nullptr};
+    static const sage_rope_plan none = {};
+    const sage_rope_plan &plan = rope ? *rope : none;
+    const int64_t tiles = bt.q_start ? bt.T / kBlock + 2 * (int64_t)bt.B : (int64_t)bt.B * (cdiv(bt.n, kBlock) + 1);
+    const dim3 grid((unsigned)tiles, 2 * c.Hkv), block(2 * c.d);
+    const bool bf16 = c.dt == SAGE_BF16, e4m3 = c.fmt == SAGE_CACHE_E4M3;
+    if (c.d == 128)
+        (bf16 ? e4m3 ? append_kernel<128, true, true> : append_kernel<128, true, false>
+              : e4m3 ? append_kernel<128, false, true> : append_kernel<128, false, false>)<<<grid, block, 0, stream>>>(a, plan);
+    else
+        (bf16 ? e4m3 ? append_kernel<64, true, true> : append_kernel<64, true, false>
+              : e4m3 ? append_kernel<64, false, true> : append_kernel<64, false, false>)<<<grid, block, 0, stream>>>(a, plan);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_gather(const sage_page_table &pt, const sage_cache &c, void *k_out, void *v_out, const Batch &bt,
+                               hipStream_t stream) {
+    GatherArgs a{pt, c, static_cast<uint16_t *>(k_out), static_cast<uint16_t *>(v_out), bt};
+    const int64_t tiles = bt.T / kBlock + (int64_t)bt.B;
+    const dim3 grid((unsigned)tiles, 2 * c.Hkv), block(2 * c.d);
+    const bool bf16 = c.dt == SAGE_BF16, e4m3 = c.fmt == SAGE_CACHE_E4M3;
+    if (c.d == 128)
+        (bf16 ? e4m3 ? gather_kernel<128, true, true> : gather_kernel<128, true, false>
+              : e4m3 ? gather_kernel<128, false, true> : gather_kernel<128, false, false>)<<<grid, block, 0, stream>>>(a);
+    else
+        (bf16 ? e4m3 ? gather_kernel<64, true, true> : gather_kernel<64, true, false>
+              : e4m3 ? gather_kernel<64, false, true> : gather_kernel<64, false, false>)<<<grid, block, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const sage_page_table &pt, const sage_cache &c, const int32_t *page_moves, int n_moves, const int32_t *slot_moves,
+                             int n_slot_moves, hipStream_t stream) {
+    const int64_t page = (int64_t)c.Hkv * pt.page_tokens * c.d, scales = (int64_t)c.Hkv * (pt.page_tokens / kBlock) * 4;
+    const int64_t tail = (int64_t)c.Hkv * kTail * c.d * 2;
+    CopyArgs a{{c.k, c.v, reinterpret_cast<uint8_t *>(c.k_scale), reinterpret_cast<uint8_t *>(c.v_scale)},
+               {page, page, scales, scales},
+               {static_cast<uint8_t *>(c.k_tail), static_cast<uint8_t *>(c.v_tail)},
+               tail, page_moves, slot_moves, n_moves, pt.n_pages, pt.slots, 1};
+    const int64_t moves = (int64_t)n_moves + n_slot_moves;
+    a.chunks = (int)std::min<int64_t>(std::max<int64_t>(1, std::max(page, tail) / (4 * 4096)), std::max<int64_t>(1, (1 << 22) / moves));
+    copy_kernel<<<dim3((unsigned)(moves * a.chunks)), dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace sage

@@ -1,0 +1,194 @@
+"""The host side of the paged cache and the rotary positions: plans against their formulas, sizes, and every refusal, without a GPU."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2505_21136_amd as sage
+from paper_2505_21136_amd import paged
+from paged_ref import Table, byte_of, quantise
+
+EINVAL, EWS, OK = -1, -2, 0
+
+
+def _freqs(rot, base, scaling, factor, trained, low, high):
+    if scaling == "ntk":
+        base = base * factor ** (rot / (rot - 2))
+    f = [base ** (-2 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    if scaling == "yarn":
+        dim = lambda t: rot * math.log(trained / (2 * math.pi * t)) / (2 * math.log(base))  # noqa: E731
+        a, b = max(math.floor(dim(high)), 0), min(math.ceil(dim(low)), rot - 1)
+        f = [x * (1 - g) + x / factor * g for i, x in enumerate(f) for g in [min(max((i - a) / max(b - a, 0.001), 0), 1)]]
+    if scaling == "bands":
+        f = [x * g + x / factor * (1 - g) for x in f for g in [min(max((trained * x / (2 * math.pi) - low) / (high - low), 0), 1)]]
+    return f
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "yarn", "bands"])
+@pytest.mark.parametrize("rot", [16, 48, 64, 128])
+@pytest.mark.parametrize("factor", [0.5, 8.0])
+def test_plan_holds_the_formulas_turns(scaling, rot, factor):
+    plan = sage.rope_plan(rot, base=50000.0, scaling=scaling, factor=factor, trained_len=4096)
+    want = _freqs(rot, 50000.0, scaling, factor, 4096, 1.0, 32.0 if scaling == "yarn" else 4.0)
+    assert plan.rot == rot and plan.layout == 0
+    for i, f in enumerate(want):
+        turns = f / (2 * math.pi) % 1.0
+        # two binary64 results of a few operations each: 16 roundings of 2^-53, relative; a plan holds whole multiples of 2^-64, the nearest
+        # of which is 2^-65 off at most
+        assert abs(plan.turns[i] / 2.0 ** 64 - turns) <= 2.0 ** -49 * max(turns, f / (2 * math.pi)) + 2.0 ** -65, (i, plan.turns[i] / 2.0 ** 64, turns)
+    assert all(plan.turns[i] == 0 for i in range(rot // 2, 64))
+    assert plan.magnitude == (pytest.approx(0.1 * math.log(factor) + 1, rel=1e-6) if scaling == "yarn" else 1.0)
+    assert sage.rope_plan(rot, scaling=scaling, factor=factor, trained_len=4096, magnitude=0.75).magnitude == 0.75
+
+
+def test_plan_refusals():
+    for bad in (dict(rot=0), dict(rot=8), dict(rot=24), dict(rot=144), dict(rot=-16), dict(base=1.0), dict(base=float("nan")), dict(base=float("inf")),
+                dict(factor=0.0), dict(factor=-1.0), dict(factor=float("inf")), dict(magnitude=-1.0), dict(magnitude=float("nan")),
+                dict(scaling="yarn", trained_len=0), dict(scaling="bands", trained_len=0), dict(scaling="bands", trained_len=10, low=4.0, high=4.0),
+                dict(scaling="yarn", trained_len=10, low=0.0), dict(layout="pairs"), dict(scaling="other"), dict(scaling="ntk", factor=1e-300)):
+        with pytest.raises(sage.SageError):
+            sage.rope_plan(bad.pop("rot", 64), **bad)
+    assert sage.lib().sage_rope_init(None, 64, 0, 0, 1e4, 1.0, 0, 1.0, 4.0, 0.0) == EINVAL
+
+
+def test_block_layout_is_a_permutation():
+    for which in "kv":
+        for d in (64, 128):
+            assert sorted(byte_of(which, r, c, d) for r in range(64) for c in range(d)) == list(range(64 * d))
+
+
+def test_quantiser_of_the_oracle_side():
+    x = torch.tensor([[1.0, -2.0] * 32]).numpy()
+    codes, scale = quantise(x, "int8")
+    assert codes[0, 1] == 1 and codes[0, 0] == 192 and codes[1, 0] == 128 and abs(scale - 2 / 127) < 1e-9   # 63.5 goes to the even 64
+    codes, scale = quantise(x, "e4m3")
+    assert codes[0, 1:2].view(torch.float8_e4m3fn).float() == -448 and codes[1, 0] == 0
+    assert quantise(x * 0, "int8")[1] == 0 and math.isnan(quantise(x * float("inf"), "e4m3")[1])
+
+
+def _structs(**change):
+    buf = (ctypes.c_char * 4096)()
+    p = (ctypes.addressof(buf) + 255) & ~255          # never dereferenced: the checks fail first
+    t = dict(table=p, lens=p, refs=p, slots=8, width=4, n_pages=16, page_tokens=128)
+    c = dict(k=p, v=p, k_scale=p, v_scale=p, k_tail=p, v_tail=p, k_shift=None, Hkv=2, d=128, fmt=0, dt=1)
+    t.update({k: v for k, v in change.items() if k in t})
+    c.update({k: v for k, v in change.items() if k in c})
+    pt, ca = paged._PageTable(**t), paged._Cache(**c)
+    return buf, p, pt, ca
+
+
+BAD_TABLES = [dict(table=None), dict(lens=None), dict(refs=None), dict(slots=0), dict(slots=4097), dict(width=0), dict(n_pages=0),
+              dict(n_pages=(1 << 22) + 1), dict(page_tokens=0), dict(page_tokens=32), dict(page_tokens=96), dict(page_tokens=65600),
+              dict(width=1 << 16)]
+BAD_CACHES = [dict(k=None), dict(v=None), dict(k_scale=None), dict(v_tail=None), dict(Hkv=0), dict(Hkv=1025), dict(d=96), dict(fmt=2), dict(dt=2)]
+
+
+@pytest.mark.parametrize("bad", BAD_TABLES + BAD_CACHES, ids=str)
+def test_bad_tables_and_caches_are_refused_everywhere(bad):
+    L = sage.lib()
+    buf, p, pt, ca = _structs(**bad)
+    r, s = ctypes.byref(pt), ctypes.byref(ca)
+    assert L.sage_paged_append(r, s, p, p, None, None, None, None, 4, 4, None, None) == EINVAL
+    assert L.sage_paged_gather(r, s, p, p, p, None, 4, 4, None) == EINVAL
+    assert L.sage_attn_fwd_paged(p, p, None, None, r, s, None, None, 4, 4, 8, 512, 1, 0.0, 0, None, None, 0) == EINVAL
+    assert L.sage_pages_copy(r, s, p, 1, None, 0, None) == EINVAL
+    if bad in BAD_TABLES:
+        assert L.sage_pages_reserve(r, p, None, 1, p, None) == EINVAL
+        assert L.sage_pages_fork(r, p, p, 1, p, p, p, None) == EINVAL
+        assert L.sage_pages_free(r, p, 1, None) == EINVAL
+        assert L.sage_pages_compact(r, p, 1, p, None, p, 1 << 30) == EINVAL
+
+
+def test_refusals_of_the_calls():
+    L = sage.lib()
+    buf, p, pt, ca = _structs()
+    r, s = ctypes.byref(pt), ctypes.byref(ca)
+    st = lambda *x: ctypes.addressof(keep.setdefault(x, (ctypes.c_int64 * 2)(*x)))  # noqa: E731
+    keep = {}
+
+    def attn(q=p, out=p, qs=None, os_=None, q_start=None, slots=None, B=4, T=4, Hq=8, max_len=512, split=64, ws=None, wsb=0):
+        return L.sage_attn_fwd_paged(q, out, qs, os_, r, s, q_start, slots, B, T, Hq, max_len, 1, 0.0, split, None, ws, wsb)
+
+    assert attn() == EWS and attn(ws=p, wsb=16) == EWS and attn(ws=p + 16, wsb=1 << 30) == EWS     # a valid call reaches the workspace check
+    for bad in (dict(q=None), dict(q=p + 8), dict(out=None), dict(B=0), dict(T=0), dict(B=3), dict(B=9, T=9), dict(Hq=7), dict(Hq=0), dict(max_len=0),
+                dict(max_len=(1 << 22) + 1), dict(split=-64), dict(split=32), dict(q_start=p + 2), dict(slots=p + 1), dict(qs=st(-8, 128)),
+                dict(qs=st(1024, 4)), dict(qs=st(1 << 41, 128)), dict(os_=st(1024, 64)), dict(os_=st(512, 128)), dict(os_=st(0, 128)),
+                dict(T=(1 << 22) + 4), dict(T=1 << 22, max_len=1 << 22)):
+        assert attn(**bad) == EINVAL, bad
+    assert attn(q_start=p, B=3) == EWS and attn(slots=p, B=64, T=64) == EWS and attn(qs=st(0, 0)) == EWS and attn(os_=st(128, 512)) == EWS
+    assert sage.paged_workspace_bytes(4, 4, 8, 2, 128, 512, 512) == 0           # one range: none needed
+    assert sage.paged_workspace_bytes(4, 4, 8, 2, 128, 512, 64) == 8 * 4 * 8 * (128 + 2) * 4
+    assert sage.paged_workspace_bytes(4, 4, 7, 2, 128, 512, 64) == 0 and sage.paged_workspace_bytes(4, 4, 8, 2, 96, 512, 64) == 0
+    for T, B, Hq, Hkv, n in ((1, 1, 1, 1, 1), (64, 64, 32, 8, 8192), (2, 2, 32, 8, 1500), (4096, 1, 32, 8, 32768), (20, 4, 128, 8, 1 << 22)):
+        k = sage.paged_split_keys(T, B, Hq, Hkv, n)
+        assert k % 64 == 0 and k >= 256
+        ranges = -(-n // k)
+        ws = sage.paged_workspace_bytes(T, B, Hq, Hkv, 64, n)
+        assert ws % 256 == 0 and (ws == 0) == (ranges == 1) and ws >= (ranges > 1) * ranges * T * Hq * 66 * 4
+
+    plan = ctypes.byref(sage.rope_plan(64))
+
+    def append(k=p, v=p, ks=None, vs=None, q_start=None, slots=None, B=4, T=4, rope=plan):
+        return L.sage_paged_append(r, s, k, v, ks, vs, q_start, slots, B, T, rope, None)
+
+    for bad in (dict(k=None), dict(v=p + 4), dict(ks=st(-8, 0)), dict(vs=st(256, 12)), dict(q_start=p + 2), dict(B=0), dict(T=0), dict(T=5), dict(B=9, T=9),
+                dict(T=1 << 23), dict(rope=ctypes.byref(paged._RopePlan()))):
+        assert append(**bad) == EINVAL, bad
+    buf64, p64, pt64, ca64 = _structs(d=64)
+    big = ctypes.byref(sage.rope_plan(128))
+    assert L.sage_paged_append(ctypes.byref(pt64), ctypes.byref(ca64), p, p, None, None, None, None, 4, 4, big, None) == EINVAL   # 128 of 64 channels
+
+    def gather(k=p, v=p, k_start=p, B=4, total=4, slots=None):
+        return L.sage_paged_gather(r, s, k, v, k_start, slots, B, total, None)
+
+    for bad in (dict(k=None), dict(v=None), dict(k=p + 2), dict(k_start=None), dict(B=0), dict(total=0), dict(total=1 << 23), dict(B=9)):
+        assert gather(**bad) == EINVAL, bad
+
+    def rope(q=p, qo=p, k=p, ko=p, pos=p, T=4, Hq=8, Hkv=2, d=128, qs=None, qos=None, ks=None, kos=None, plan=plan, dt=0):
+        return L.sage_rope(q, qo, k, ko, pos, T, Hq, Hkv, d, qs, qos, ks, kos, plan, 0, dt, None)
+
+    for bad in (dict(q=None), dict(qo=None), dict(pos=None), dict(k=None), dict(ko=None), dict(Hkv=0), dict(Hkv=-1), dict(Hq=0), dict(Hq=4095), dict(T=0),
+                dict(T=(1 << 22) + 1), dict(d=96), dict(dt=2), dict(plan=None), dict(plan=ctypes.byref(paged._RopePlan())), dict(d=64, plan=big),
+                dict(q=p + 2), dict(qs=st(0, 1024)), dict(qos=st(1024, 64)), dict(kos=st(0, 128)), dict(kos=st(120, 128)), dict(qs=st(8, -8))):
+        assert rope(**bad) == EINVAL, bad
+
+    for n in (0, 4097, -1):
+        assert L.sage_pages_reserve(r, p, None, n, p, None) == EINVAL
+        assert L.sage_pages_fork(r, p, p, n, p, p, p, None) == EINVAL
+        assert L.sage_pages_free(r, p, n, None) == EINVAL
+    assert L.sage_pages_reserve(r, None, None, 1, p, None) == EINVAL and L.sage_pages_reserve(r, p, None, 1, None, None) == EINVAL
+    assert L.sage_pages_fork(r, p, p, 1, p, None, p, None) == EINVAL and L.sage_pages_free(r, None, 1, None) == EINVAL
+    assert L.sage_pages_compact(r, p, 0, p, None, p, 1 << 20) == EINVAL and L.sage_pages_compact(r, None, 1, p, None, p, 1 << 20) == EINVAL
+    assert L.sage_pages_compact(r, p, 1, p, None, None, 1 << 20) == EWS and L.sage_pages_compact(r, p, 1, p, None, p, 16) == EWS
+    assert L.sage_pages_compact_workspace_bytes(0) == 0 and L.sage_pages_compact_workspace_bytes(65) == 512
+    assert L.sage_pages_copy(r, s, p, 0, None, 0, None) == EINVAL and L.sage_pages_copy(r, s, None, 1, None, 0, None) == EINVAL
+    assert L.sage_pages_copy(r, s, p, -1, p, 1, None) == EINVAL and L.sage_pages_copy(r, s, p, 1, p, 4097, None) == EINVAL
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes():
+    x = torch.zeros(4, 2, 64, dtype=torch.float16)
+    plan = sage.rope_plan(64)
+    with pytest.raises(sage.SageError):
+        sage.sage_rope(x, torch.zeros(4, dtype=torch.int32), plan)
+    with pytest.raises(sage.SageError):
+        sage.PageTable.empty(4, page_tokens=64, slots=2, width=2, device="cpu")
+
+
+def test_table_simulation_is_consistent():
+    class Pages:
+        page_tokens, width = 64, 4
+        table = torch.full((6, 4), -1, dtype=torch.int32)
+        lens = torch.zeros(6, dtype=torch.int32)
+        refs = torch.zeros(9, dtype=torch.int32)
+
+    t = Table(Pages)
+    assert t.reserve([2, 0, 2, 7, 1], [130, 1, 1, 1, 300]) == [0, 0, -1, -1, -1]
+    assert t.table[2] == [0, 1, 2, -1] and t.table[0] == [3, -1, -1, -1] and t.lens[2] == 130
+    assert t.fork([2, 2, 0], [3, 4, 4])[0] == [0, 0, -1] and t.refs == t.count()
+    t.free([2, 2])
+    assert t.refs == t.count() and t.lens[2] == 0
+    t.compact(9)
+    assert t.refs == t.count() and all(r > 0 for r in t.refs[:sum(x > 0 for x in t.refs)])
