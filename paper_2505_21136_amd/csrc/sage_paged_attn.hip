@@ -6,10 +6,10 @@
 //
 // The cache keeps the bytes of a block in the order of the operands, so a wavefront loads 1 KB of neighbouring bytes at a time
 // straight into registers; nothing of K, V or P passes through LDS and the loop has no barrier.  The rows of all query heads that share a
-// K/V head are packed, token by token, into tiles of 16: the cache of a head is read once for all of them.
+// K/V head are packed, token by token, into tiles of 16 or 32: the cache of a head is read once for all of them.
 //
-// A workgroup is four wavefronts.  One with up to 16 NT rows shares its keys among them (wavefront w takes every fourth block; the
-// partial sums meet in LDS at the end), one with more gives each wavefront, or each two, rows of their own.
+// A workgroup is four wavefronts of 16 or 32 rows.  With no more rows than one wavefront takes, the four share the keys (wavefront w takes
+// every fourth block; the partial sums meet in LDS at the end); with more, each wavefront, or each two, have rows of their own.
 #include "sage_paged.h"
 
 #include <algorithm>
@@ -58,6 +58,14 @@ __device__ __forceinline__ v8h codes_to_half(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(v8h, v4u{w[0], w[1], w[2], w[3]});
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
+// Two weights as binary16, rounded to nearest even in one instruction.
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, v2h));
+}
+#endif
+
 // A row's running sums on their way into the output or the workspace.
 template <int D, bool BF16>
 __device__ __forceinline__ void store_row_quad(const PagedArgs &a, int tok, int hq, int ch, const float4 &acc, float l, bool split, int s) {
@@ -71,15 +79,38 @@ __device__ __forceinline__ void store_row_quad(const PagedArgs &a, int tok, int 
     }
 }
 
-// D: head dimension; NT: row tiles of 16 per wavefront.
-template <int D, bool BF16, bool E4M3, int NT>
-__global__ __launch_bounds__(64 * kAttnWaves, NT == 1 ? 2 : 1) void paged_rows_kernel(const PagedArgs a) {
+// The matrix instruction for M query rows: M = 16 (16x16x32) or 32 (32x32x16).  Of an accumulator tile a lane holds, for row lane % M, the
+// elements 8 * (i >> 2) + 4 * (lane / M) + (i & 3), i < M * M / 64.
+template <int M>
+struct Mfma;
+template <>
+struct Mfma<16> {
+    typedef v4f acc;
+    static __device__ __forceinline__ acc run(v8h a, v8h b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float row_max(float x) { return rowgroup_max(x); }
+    static __device__ __forceinline__ float row_sum(float x) { return rowgroup_sum(x); }
+};
+template <>
+struct Mfma<32> {
+    typedef float acc __attribute__((ext_vector_type(16)));
+    static __device__ __forceinline__ acc run(v8h a, v8h b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float row_max(float x) { return halves_max(x); }
+    static __device__ __forceinline__ float row_sum(float x) { return halves_sum(x); }
+};
+
+// D: head dimension; M: rows per wavefront, 16 or 32.
+template <int D, bool BF16, bool E4M3, int M>
+__global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int C = D / 64, CT = D / 16, ROWS = 16 * NT * kAttnWaves, LD = D + 4;
+    constexpr int NL = D / 16;       // loads of 16 bytes a lane for a block of K, and of V
+    constexpr int R = M * M / 64;    // registers of an accumulator tile
+    constexpr int KT = 64 / M, OT = D / M, NP = KT * R, ROWS = M * kAttnWaves, LD = D + 4;
+    constexpr int QS = D / (512 / M); // matrix instructions that a key tile's scores take (8 channels a lane each)
+    typedef typename Mfma<M>::acc acc_t;
     __shared__ int found[2];
-    __shared__ __attribute__((aligned(16))) float acc_lds[kAttnWaves * 16 * NT * LD];
-    __shared__ float2 ml_lds[kAttnWaves * 16 * NT];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane & 15, g = lane >> 4;
+    __shared__ __attribute__((aligned(16))) float acc_lds[kAttnWaves * M * LD];
+    __shared__ float2 ml_lds[kAttnWaves * M];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane % M, g = lane / M;
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv, split = blockIdx.y;
     int b, tile;
     if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
@@ -91,73 +122,61 @@ __global__ __launch_bounds__(64 * kAttnWaves, NT == 1 ? 2 : 1) void paged_rows_k
     const int cap = a.pt.width * a.pt.page_tokens, true_len = max(a.pt.lens[slot], 0), len = min(true_len, cap);
 
     // ---- this wavefront's rows and blocks ----
-    const int RW = rows > 32 * NT ? 4 : rows > 16 * NT ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
+    const int RW = rows > 2 * M ? 4 : rows > M ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
     const int rg = wave % RW, kg = wave / RW;
-    const int first = tile * ROWS + rg * 16 * NT;              // packed row of this wavefront's first
-    const int mine = min(rows - rg * 16 * NT, 16 * NT);        // rows of this wavefront, may be <= 0
+    const int first = tile * ROWS + rg * M;         // packed row of this wavefront's first
+    const int mine = min(rows - rg * M, M);         // rows of this wavefront, may be <= 0
     // the last key that packed row ri sees
     const auto last_key = [&](int ri) { return a.causal ? min(len - 1, len - n + ri / a.group) : len - 1; };
     const int lim_lo = last_key(first), lim_hi = mine > 0 ? last_key(first + mine - 1) : -1;
     int jb = split * a.split_blocks, je = lim_hi < 0 ? 0 : lim_hi / kBlock + 1;
     if (split + 1 < a.splits) je = min(je, jb + a.split_blocks);
 
-    // ---- Q ----
-    v8h qh[NT][C][2];
-    float row_scale[NT];
-    int lim[NT];
-    float m[NT], l[NT];
-    v4f o[NT][CT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int ri = min(first + min(16 * t + lq, max(mine, 1) - 1), n * a.group - 1), tok = ri / a.group, hq = kvh * a.group + ri % a.group;
-        lim[t] = last_key(ri);
-        m[t] = -INFINITY, l[t] = 0.0f;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[t][ct] = v4f{0.f, 0.f, 0.f, 0.f};
+    // ---- Q: run i of 8 channels a lane ----
+    v8h qh[QS];
+    float row_scale;
+    const int ri0 = min(first + min(lq, max(mine, 1) - 1), n * a.group - 1);
+    const int lim = last_key(ri0);
+    {
+        const int tok = ri0 / a.group, hq = kvh * a.group + ri0 % a.group;
         const uint16_t *p = a.q + (int64_t)(q0 + tok) * a.q_st.t + hq * a.q_st.h + 16 * g;
-        uint4 x[C][2];
+        uint4 x[QS];
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) x[c][e] = *reinterpret_cast<const uint4 *>(p + 64 * c + 8 * e);
+        for (int i = 0; i < QS; ++i) x[i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
         float s = 1.0f;
+        row_scale = a.scale;
         if constexpr (BF16) {
             // binary16 has bfloat16's precision and more, not its range: the row is brought to 1 .. 2 by a power of two
             float top = 0.0f;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int i = 0; i < QS; ++i) {
+                float f[8];
+                unpack8<true>(x[i], f);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float f[8];
-                    unpack8<true>(x[c][e], f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
-                }
-            top = rowgroup_max(top);
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+            }
+            top = Mfma<M>::row_max(top);
             const int ex = min(max((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127, -126), 126);
             s = __builtin_bit_cast(float, (uint32_t)(127 - ex) << 23);
-            row_scale[t] = __builtin_bit_cast(float, (uint32_t)(127 + ex) << 23) * a.scale;
-        } else {
-            row_scale[t] = a.scale;
+            row_scale *= __builtin_bit_cast(float, (uint32_t)(127 + ex) << 23);
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if constexpr (BF16) {
-                    float f[8];
-                    unpack8<true>(x[c][e], f);
-                    uint4 w;
-                    w.x = pack2<false>(f[0] * s, f[1] * s), w.y = pack2<false>(f[2] * s, f[3] * s);
-                    w.z = pack2<false>(f[4] * s, f[5] * s), w.w = pack2<false>(f[6] * s, f[7] * s);
-                    qh[t][c][e] = __builtin_bit_cast(v8h, w);
-                } else {
-                    qh[t][c][e] = __builtin_bit_cast(v8h, x[c][e]);
-                }
+        for (int i = 0; i < QS; ++i) {
+            if constexpr (BF16) {
+                float f[8];
+                unpack8<true>(x[i], f);
+                const uint4 w = make_uint4(pack_half(f[0] * s, f[1] * s), pack_half(f[2] * s, f[3] * s),
+                                           pack_half(f[4] * s, f[5] * s), pack_half(f[6] * s, f[7] * s));
+                qh[i] = __builtin_bit_cast(v8h, w);
+            } else {
+                qh[i] = __builtin_bit_cast(v8h, x[i]);
             }
+        }
     }
-    const int tiles_here = mine > 0 ? (mine + 15) >> 4 : 0;
-    float vref = 0.0f;  // the largest V scale so far: o stands for o * vref
+    float m = -INFINITY, l = 0.0f, vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
+    acc_t o[OT];
+#pragma unroll
+    for (int i = 0; i < OT; ++i) o[i] = acc_t{};
 
     // ---- the keys, block by block ----
     const int per_page = a.pt.page_tokens / kBlock;
@@ -167,173 +186,184 @@ __global__ __launch_bounds__(64 * kAttnWaves, NT == 1 ? 2 : 1) void paged_rows_k
         blk = ((size_t)max(page, 0) * a.Hkv + kvh) * per_page + (page < 0 ? 0 : in_page);
         return page >= 0;
     };
-    const auto load = [&](uint4 *x, const uint8_t *pool, size_t blk) {
-        const uint8_t *p = pool + blk * (kBlock * D) + 16 * lane;
+    // M = 16: load i is the i-th KB of the block.  M = 32: a lane takes its place in KB pairs, halves of 512 bytes at a time: of K key tile
+    // i / (2 D/64), channels 64 (i / 2 % (D/64)) + 32 (i & 1) + 16 g ..; of V channels 32 (i / 2) .., tokens 16 w + 8 (i & 1) + 4 g ..
+    const int k_lane = M == 16 ? 16 * lane : (lane >> 4 & 1) * (D / 64) * 1024 + 256 * g + 16 * (lane & 15);
+    const int v_lane = M == 16 ? 16 * lane : (lane >> 4 & 1) * 1024 + 256 * g + 16 * (lane & 15);
+    const auto k_at = [](int i) { return M == 16 ? 1024 * i : (i / (D / 32)) * (D / 64) * 2048 + (i / 2 % (D / 64)) * 1024 + 512 * (i & 1); };
+    const auto v_at = [](int i) { return M == 16 ? 1024 * i : 2048 * (i >> 1) + 512 * (i & 1); };
+    uint4 kx[NL], vx[NL];
+    const auto load_k = [&](size_t blk) {
+        const uint8_t *p = a.k + blk * (kBlock * D) + k_lane;
 #pragma unroll
-        for (int i = 0; i < CT; ++i) x[i] = *reinterpret_cast<const uint4 *>(p + 1024 * i);
+        for (int i = 0; i < NL; ++i) kx[i] = *reinterpret_cast<const uint4 *>(p + k_at(i));
     };
-    uint4 kx[CT], vx[CT];  // (4 C = CT)
+    const auto load_v = [&](size_t blk) {
+        const uint8_t *p = a.v + blk * (kBlock * D) + v_lane;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) vx[i] = *reinterpret_cast<const uint4 *>(p + v_at(i));
+    };
     size_t blk = 0;
     float ks = 0.0f, vs = 0.0f;
     const auto scales_of = [&](bool there) {
         ks = there ? a.k_scale[blk] : __builtin_nanf("");
         vs = there ? a.v_scale[blk] : __builtin_nanf("");
     };
+
+    acc_t s[KT];
+    v8h pb[NP / 8];
+    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far; MASKED: some row does not see
+    // some key of the block.
+    const auto softmax = [&](auto masked_c, int key0) {
+        constexpr bool MASKED = decltype(masked_c)::value;
+        const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim; };
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < R; ++i) s[t][i] = hidden(t, i) ? -INFINITY : s[t][i];
+        }
+        const float c = row_scale * ks;  // >= 0, so the order of the scores is that of the sums
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < R; ++i) top = fmaxf(top, s[t][i]);
+        const float m_new = fmaxf(m, Mfma<M>::row_max(top) * c);
+        const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
+        const float alpha = __builtin_amdgcn_exp2f(m - base);
+        // V's scale goes into the exponent (a block of zeros: any will do)
+        const float vnew = fmaxf(vref, vs), back = vnew > 0.0f ? vref * __builtin_amdgcn_rcpf(vnew) : 0.0f;
+        const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
+        const float shift = (vs == vs ? lr : vs) - base;
+        float sum = 0.0f;
+#pragma unroll
+        for (int st = 0; st < NP / 8; ++st) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = (8 * st + e) / R, i = (8 * st + e) % R;
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, shift));
+                if constexpr (MASKED) p[e] = hidden(t, i) ? 0.0f : p[e];  // (and no NaN of the scales comes in)
+                sum += p[e];
+            }
+            const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
+            pb[st] = __builtin_bit_cast(v8h, w);
+        }
+        l = l * alpha + sum * __builtin_amdgcn_exp2f(-lr);
+        m = m_new;
+        vref = vnew;
+        return alpha * back;  // what o is to be multiplied by
+    };
+
     jb += kg;
     if (jb < je) {
         const bool there = block_at(jb, blk);
-        load(kx, a.k, blk);
-        load(vx, a.v, blk);
+        load_k(blk);
+        load_v(blk);
         scales_of(there);
     }
     for (int j = jb; j < je; j += KW) {
         const int next = j + KW < je ? j + KW : j;  // (the last one loads its own block again: no branch around the loads)
         size_t nblk;
         const bool there = block_at(next, nblk);
-        v4f s[NT][4];
 #pragma unroll
-        for (int t4 = 0; t4 < 4; ++t4)
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const uint4 x = kx[t4 * C + c];
-                const v8h k0 = codes_to_half<E4M3>(x.x, x.y), k1 = codes_to_half<E4M3>(x.z, x.w);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (NT > 1 && t >= tiles_here) continue;
-                    const v4f zero = {0.f, 0.f, 0.f, 0.f};
-                    s[t][t4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[t][c][0], c == 0 ? zero : s[t][t4], 0, 0, 0);
-                    s[t][t4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[t][c][1], s[t][t4], 0, 0, 0);
-                }
+            for (int i = 0; i < QS / 2; ++i) {
+                const uint4 x = kx[t * (QS / 2) + i];
+                s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), qh[2 * i], i == 0 ? acc_t{} : s[t]);
+                s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), qh[2 * i + 1], s[t]);
+                if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
             }
-        load(kx, a.k, nblk);
-
-        // ---- softmax step ----
-        const int key0 = j * kBlock;
-        const bool masked = key0 + kBlock - 1 > lim_lo;
-        const float vnew = fmaxf(vref, vs), back = vnew > 0.0f ? vref / vnew : 0.0f, ratio = vs == 0.0f ? 0.0f : vs / vnew;
-        v8h pb[NT][2];
+        load_k(nblk);
+        const float f = j * kBlock + kBlock - 1 > lim_lo ? softmax(std::true_type{}, j * kBlock) : softmax(std::false_type{}, 0);
+        if (__builtin_amdgcn_ballot_w64(f != 1.0f) != 0) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (NT > 1 && t >= tiles_here) continue;
-            const float c = row_scale[t] * ks;
-            float top = -INFINITY;
+            for (int i = 0; i < OT; ++i) o[i] *= f;
+        }
+        // O^T += V^T P^T
 #pragma unroll
-            for (int t4 = 0; t4 < 4; ++t4)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = s[t][t4][i] * c;
-                    if (masked && key0 + 16 * t4 + 4 * g + i > lim[t]) x = -INFINITY;
-                    s[t][t4][i] = x;
-                    top = fmaxf(top, x);
-                }
-            const float m_new = fmaxf(m[t], rowgroup_max(top));
-            const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
-            const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
-            float sum = 0.0f, p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(s[t][i >> 2][i & 3] - base);
-                sum += p[i];
-            }
-            l[t] = l[t] * alpha + sum;
-            m[t] = m_new;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] *= ratio;
-                // (a key that the row does not see must not bring the scale's NaN in)
-                if (masked && key0 + 16 * (i >> 2) + 4 * g + (i & 3) > lim[t]) p[i] = 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint4 w = make_uint4(pack2<false>(p[8 * u], p[8 * u + 1]), pack2<false>(p[8 * u + 2], p[8 * u + 3]),
-                                           pack2<false>(p[8 * u + 4], p[8 * u + 5]), pack2<false>(p[8 * u + 6], p[8 * u + 7]));
-                pb[t][u] = __builtin_bit_cast(v8h, w);
-            }
-            const float f = alpha * back;
-            if (__builtin_amdgcn_ballot_w64(f != 1.0f) != 0) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) o[t][ct] *= f;
+        for (int t = 0; t < OT; ++t) {
+            if constexpr (M == 16) {
+                const uint4 x = vx[t];
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), pb[0], o[t]);
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), pb[1], o[t]);
+            } else {
+                const uint4 x = vx[2 * t], y = vx[2 * t + 1];
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, y.x), pb[0], o[t]);
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.y, y.y), pb[1], o[t]);
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, y.z), pb[2], o[t]);
+                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.w, y.w), pb[3], o[t]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        vref = vnew;
-
-        // ---- O^T += V^T P^T ----
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const uint4 x = vx[ct];
-            const v8h v0 = codes_to_half<E4M3>(x.x, x.y), v1 = codes_to_half<E4M3>(x.z, x.w);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (NT > 1 && t >= tiles_here) continue;
-                o[t][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pb[t][0], o[t][ct], 0, 0, 0);
-                o[t][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pb[t][1], o[t][ct], 0, 0, 0);
-            }
-        }
-        load(vx, a.v, nblk);
+        load_v(nblk);
         blk = nblk;
         scales_of(there);
     }
     // a length beyond the table's row: what the row cannot hold is missing
-    const float poison = true_len > cap ? __builtin_nanf("") : 0.0f;
+    const float sum = Mfma<M>::row_sum(l) + (true_len > cap ? __builtin_nanf("") : 0.0f);
 
     // ---- the key groups' sums ----
     const bool to_workspace = a.splits > 1;
+    if (KW == 1) {
+        if (lq >= mine) return;
+        const int ri = first + lq, tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
+        if (to_workspace && g == 0)
+            *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(m, sum);
+        if (to_workspace && m == -INFINITY && sum == 0.0f) return;  // (the combination does not read it)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        if (t >= tiles_here) continue;
-        const float sum = rowgroup_sum(l[t]) + poison;
-        if (KW == 1) {
-            if (16 * t + lq >= mine) continue;
-            const int ri = first + 16 * t + lq, tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
-            if (to_workspace && g == 0)
-                *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(m[t], sum);
-            if (to_workspace && m[t] == -INFINITY && sum == 0.0f) continue;  // (the combination does not read it)
+        for (int t = 0; t < OT; ++t)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const v4f y = o[t][ct] * vref;
-                store_row_quad<D, BF16>(a, tok, hq, 16 * ct + 4 * g, make_float4(y[0], y[1], y[2], y[3]), sum, to_workspace, split);
-            }
-        } else {
-            const int r = wave * 16 * NT + 16 * t + lq;
-            if (g == 0) ml_lds[r] = make_float2(m[t], sum);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const v4f y = o[t][ct] * vref;
-                *reinterpret_cast<float4 *>(acc_lds + r * LD + 16 * ct + 4 * g) = make_float4(y[0], y[1], y[2], y[3]);
-            }
-        }
+            for (int i = 0; i < R; i += 4)
+                store_row_quad<D, BF16>(a, tok, hq, M * t + 2 * i + 4 * g,
+                                        make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref), sum,
+                                        to_workspace, split);
+        return;
     }
-    if (KW == 1) return;
+    {
+        const int r = wave * M + lq;
+        if (g == 0) ml_lds[r] = make_float2(m, sum);
+#pragma unroll
+        for (int t = 0; t < OT; ++t)
+#pragma unroll
+            for (int i = 0; i < R; i += 4)
+                *reinterpret_cast<float4 *>(acc_lds + r * LD + M * t + 2 * i + 4 * g) =
+                    make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref);
+    }
     __syncthreads();
     for (int e = tid; e < rows * (D / 4); e += 64 * kAttnWaves) {
-        const int r = e / (D / 4), ch = 4 * (e % (D / 4)), w0 = r / (16 * NT), rr = r % (16 * NT);
+        const int r = e / (D / 4), ch = 4 * (e % (D / 4)), w0 = r / M, rr = r % M;
         const int ri = tile * ROWS + r, tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
         float mx = -INFINITY;
-        for (int w = w0; w < kAttnWaves; w += RW) mx = fmaxf(mx, ml_lds[w * 16 * NT + rr].x);
+        for (int w = w0; w < kAttnWaves; w += RW) mx = fmaxf(mx, ml_lds[w * M + rr].x);
         const float base = mx == -INFINITY ? 0.0f : mx;
-        float sum = 0.0f;
+        float all = 0.0f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = w0; w < kAttnWaves; w += RW) {
-            const float2 ml = ml_lds[w * 16 * NT + rr];
+            const float2 ml = ml_lds[w * M + rr];
             const float f = __builtin_amdgcn_exp2f(ml.x - base);
-            const float4 y = *reinterpret_cast<const float4 *>(acc_lds + (w * 16 * NT + rr) * LD + ch);
-            sum += f * ml.y;
+            const float4 y = *reinterpret_cast<const float4 *>(acc_lds + (w * M + rr) * LD + ch);
+            all += f * ml.y;
             acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
         }
         if (to_workspace && ch == 0)
-            *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(mx, sum);
-        if (to_workspace && mx == -INFINITY && sum == 0.0f) continue;
-        store_row_quad<D, BF16>(a, tok, hq, ch, acc, sum, to_workspace, split);
+            *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(mx, all);
+        if (to_workspace && mx == -INFINITY && all == 0.0f) continue;
+        store_row_quad<D, BF16>(a, tok, hq, ch, acc, all, to_workspace, split);
     }
 #endif  // __HIP_DEVICE_COMPILE__
 }
 
-// The ranges of a row combined as partial softmax sums.  A workgroup per 16 packed rows of a K/V head; a thread owns four channels of a row.  Ranges
-// that the row sees nothing of have no sums and are passed over.
+// The ranges of a row combined as partial softmax sums.  A workgroup per 1024 / D packed rows of a K/V head, a thread per four channels of a row.
+// Bound by latency with few rows: the ranges' weights are computed by all threads at once and meet in LDS, then eight ranges' sums are
+// in flight per thread.  Ranges that the row sees nothing of have no sums; what lies in their place is not used.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a) {
-    constexpr int ROWS = 16;
+    constexpr int ROWS = 1024 / D, EACH = 256 / ROWS, CHUNK = 256;  // EACH: threads per row
     __shared__ int found[2];
+    __shared__ float weight[ROWS][CHUNK];
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv;
     int b, tile;
     if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
@@ -342,38 +372,61 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a) {
     const int slot = a.bt.slots ? a.bt.slots[b] : b;
     const int rows = min(n * a.group - tile * ROWS, ROWS);
     if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
-    for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
-        const int ri = tile * ROWS + e / (D / 4), ch = 4 * (e % (D / 4));
-        const int tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
-        const size_t row0 = (size_t)tok * a.Hq + hq, step = (size_t)a.bt.T * a.Hq;
-        float mx = -INFINITY;
-        for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, a.part_ml[2 * (row0 + s * step)]);
-        const float base = mx == -INFINITY ? 0.0f : mx;
-        float sum = 0.0f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < a.splits; ++s) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (row0 + s * step));
-            if (ml.x == -INFINITY && ml.y == 0.0f) continue;
-            const float f = __builtin_amdgcn_exp2f(ml.x - base);
-            const float4 y = *reinterpret_cast<const float4 *>(a.part_acc + (row0 + s * step) * D + ch);
-            sum += f * ml.y;
-            acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
+    const int r = threadIdx.x / EACH, e = threadIdx.x % EACH;
+    const int ri = tile * ROWS + min(r, rows - 1), tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
+    const size_t row0 = (size_t)tok * a.Hq + hq, step = (size_t)a.bt.T * a.Hq;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
+    const auto lanes = [](float x, auto op) {  // over the row's EACH lanes
+#pragma unroll
+        for (int d = 1; d < EACH; d <<= 1) x = op(x, __shfl_xor(x, d));
+        return x;
+    };
+    float mx = -INFINITY;
+    for (int s = e; s < a.splits; s += EACH) mx = fmaxf(mx, ml[row0 + s * step].x);
+    mx = lanes(mx, [](float x, float y) { return fmaxf(x, y); });
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float sum = 0.0f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < a.splits; s0 += CHUNK) {
+        const int here = min(a.splits - s0, CHUNK);
+        __syncthreads();
+        for (int s = e; s < here; s += EACH) {
+            const float2 x = ml[row0 + (s0 + s) * step];
+            const bool none = x.x == -INFINITY && x.y == 0.0f;
+            const float w = none ? 0.0f : __builtin_amdgcn_exp2f(x.x - base);
+            weight[r][s] = none ? -1.0f : w;
+            sum += w * x.y;
         }
-        store_row_quad<D, BF16>(a, tok, hq, ch, acc, sum, false, 0);
+        __syncthreads();
+        for (int s = 0; s < here; s += 8) {
+            float4 y[8];
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = min(s + i, here - 1);
+                w[i] = s + i < here ? weight[r][k] : -1.0f;
+                y[i] = *reinterpret_cast<const float4 *>(a.part_acc + (row0 + (s0 + k) * step) * D + 4 * e);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (w[i] == -1.0f) continue;
+                acc.x += w[i] * y[i].x, acc.y += w[i] * y[i].y, acc.z += w[i] * y[i].z, acc.w += w[i] * y[i].w;
+            }
+        }
     }
+    sum = lanes(sum, [](float x, float y) { return x + y; });
+    if (r < rows) store_row_quad<D, BF16>(a, tok, hq, 4 * e, acc, sum, false, 0);
 }
 
 template <int D, bool BF16, bool E4M3>
-void launch_nt(int nt, dim3 grid, hipStream_t stream, const PagedArgs &a) {
+void launch_rows(int m, dim3 grid, hipStream_t stream, const PagedArgs &a) {
     const dim3 block(64 * kAttnWaves);
-    if (nt == 1) paged_rows_kernel<D, BF16, E4M3, 1><<<grid, block, 0, stream>>>(a);
-    else paged_rows_kernel<D, BF16, E4M3, 2><<<grid, block, 0, stream>>>(a);
+    if (m == 16) paged_rows_kernel<D, BF16, E4M3, 16><<<grid, block, 0, stream>>>(a);
+    else paged_rows_kernel<D, BF16, E4M3, 32><<<grid, block, 0, stream>>>(a);
 }
 
-// Row tiles of 16 per wavefront, from the mean number of packed rows per sequence and K/V head.
-int row_tiles(int T, int B, int group) {
-    return (int64_t)T * group <= 16 * (int64_t)B ? 1 : 2;
-}
+// Rows per wavefront, from the mean number of packed rows per sequence and K/V head.
+int wave_rows(int T, int B, int group) { return (int64_t)T * group <= 16 * (int64_t)B ? 16 : 32; }
 int64_t row_slots(int T, int B, int group, int rows, bool ragged) {
     if (!ragged) return (int64_t)B * (((int64_t)(T / B) * group + rows - 1) / rows);
     return (int64_t)T * group / rows + B;
@@ -382,8 +435,8 @@ int64_t row_slots(int T, int B, int group, int rows, bool ragged) {
 }  // namespace
 
 int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
-    const int group = Hq / Hkv, nt = row_tiles(T, B, group);
-    const int64_t tiles = ((int64_t)T * group + 64 * nt * (int64_t)B - 1) / (64 * nt * (int64_t)B);  // of a sequence, at the mean
+    const int group = Hq / Hkv, rows = kAttnWaves * wave_rows(T, B, group);
+    const int64_t tiles = ((int64_t)T * group + rows * (int64_t)B - 1) / (rows * (int64_t)B);  // of a sequence, at the mean
     const int64_t workgroups = tiles * B * Hkv;
     // three workgroups per CU, ranges of at least four blocks
     const int64_t ranges = std::max<int64_t>(1, 3 * kCUs / workgroups);
@@ -403,7 +456,7 @@ PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len,
 }
 
 int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, bool ragged, int splits) {
-    return row_slots(T, B, Hq / Hkv, 16, ragged) * Hkv * splits;  // (an upper bound for both kernels)
+    return row_slots(T, B, Hq / Hkv, 8, ragged) * Hkv * splits;  // (an upper bound for both kernels)
 }
 
 hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenStrides o_st, const sage_page_table &pt, const sage_cache &c,
@@ -412,17 +465,17 @@ hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenS
     PagedArgs a{static_cast<const uint16_t *>(q), static_cast<uint16_t *>(out), q_st, o_st, pt, c.k, c.v, c.k_scale, c.v_scale, bt, Hq, c.Hkv,
                 Hq / c.Hkv, causal, split_keys / kBlock, ws.splits, (float)(sm_scale * 1.4426950408889634), ws.part_acc, ws.part_ml};
     const bool bf16 = c.dt == SAGE_BF16, e4m3 = c.fmt == SAGE_CACHE_E4M3;
-    const int nt = row_tiles(bt.T, bt.B, a.group);
-    const dim3 grid((unsigned)(row_slots(bt.T, bt.B, a.group, 64 * nt, bt.q_start != nullptr) * c.Hkv), (unsigned)ws.splits);
+    const int m = wave_rows(bt.T, bt.B, a.group);
+    const dim3 grid((unsigned)(row_slots(bt.T, bt.B, a.group, kAttnWaves * m, bt.q_start != nullptr) * c.Hkv), (unsigned)ws.splits);
     if (c.d == 128)
-        (bf16 ? e4m3 ? launch_nt<128, true, true> : launch_nt<128, true, false>
-              : e4m3 ? launch_nt<128, false, true> : launch_nt<128, false, false>)(nt, grid, stream, a);
+        (bf16 ? e4m3 ? launch_rows<128, true, true> : launch_rows<128, true, false>
+              : e4m3 ? launch_rows<128, false, true> : launch_rows<128, false, false>)(m, grid, stream, a);
     else
-        (bf16 ? e4m3 ? launch_nt<64, true, true> : launch_nt<64, true, false>
-              : e4m3 ? launch_nt<64, false, true> : launch_nt<64, false, false>)(nt, grid, stream, a);
+        (bf16 ? e4m3 ? launch_rows<64, true, true> : launch_rows<64, true, false>
+              : e4m3 ? launch_rows<64, false, true> : launch_rows<64, false, false>)(m, grid, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || ws.splits == 1) return e;
-    const dim3 mgrid((unsigned)(row_slots(bt.T, bt.B, a.group, 16, bt.q_start != nullptr) * c.Hkv));
+    const dim3 mgrid((unsigned)(row_slots(bt.T, bt.B, a.group, 1024 / c.d, bt.q_start != nullptr) * c.Hkv));
     if (c.d == 128)
         (bf16 ? paged_merge_kernel<128, true> : paged_merge_kernel<128, false>)<<<mgrid, dim3(256), 0, stream>>>(a);
     else
