@@ -21,11 +21,20 @@ struct Batch {
 
 namespace {
 
+// A load through the scalar cache, at an address that is the same for all lanes, of memory that the kernel does not write.  It is waited for
+// by itself: a vector load would be waited for in order, together with everything that was fetched ahead before it.
+__device__ __forceinline__ int32_t scalar_load(const int32_t *p) {
+    return *(const __attribute__((address_space(4))) int32_t *)(uint64_t)p;
+}
+__device__ __forceinline__ float scalar_load(const float *p) {
+    return *(const __attribute__((address_space(4))) float *)(uint64_t)p;
+}
+
 // Sequence b's rows, within 0 .. T whatever q_start holds.
 __device__ __forceinline__ void rows_of(const Batch &bt, int b, int &q0, int &n) {
     if (bt.q_start) {
-        q0 = min(max(bt.q_start[b], 0), bt.T);
-        n = max(min(max(bt.q_start[b + 1], 0), bt.T) - q0, 0);
+        q0 = min(max(scalar_load(bt.q_start + b), 0), bt.T);
+        n = max(min(max(scalar_load(bt.q_start + b + 1), 0), bt.T) - q0, 0);
     } else {
         q0 = b * bt.n, n = bt.n;
     }
@@ -55,12 +64,15 @@ __device__ __forceinline__ bool locate(const Batch &bt, int x, int rows, int per
     return b >= 0;
 }
 
+// Sequence b's slot.
+__device__ __forceinline__ int slot_of(const Batch &bt, int b) { return bt.slots ? scalar_load(bt.slots + b) : b; }
+
 // The page that holds block j (of 64 tokens) of a slot, -1 where the table has none.
 __device__ __forceinline__ int page_of(const sage_page_table &pt, int slot, int j, int per_page, int &in_page) {
     const int i = j / per_page;
     in_page = j - i * per_page;
     if (i >= pt.width) return -1;
-    const int p = pt.table[(size_t)slot * pt.width + i];
+    const int p = scalar_load(pt.table + (size_t)slot * pt.width + i);
     return p >= 0 && p < pt.n_pages ? p : -1;
 }
 

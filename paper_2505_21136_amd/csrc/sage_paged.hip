@@ -70,9 +70,9 @@ __global__ __launch_bounds__(2 * D) void append_kernel(const AppendArgs a, const
     if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 2, b, x, found)) return;
     int q0, n;
     rows_of(a.bt, b, q0, n);
-    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    const int slot = slot_of(a.bt, b);
     if (n == 0 || slot < 0 || slot >= a.pt.slots) return;
-    const int len = min(a.pt.lens[slot], a.pt.width * a.pt.page_tokens);
+    const int len = min(scalar_load(a.pt.lens + slot), a.pt.width * a.pt.page_tokens);
     const int start = max(len - n, 0);  // first new token; row q0 + p - (len - n) is token p
     const int row0 = q0 - (len - n);
     const int j0 = start / kBlock, jl = (len - 1) / kBlock, j = j0 + x;
@@ -239,17 +239,17 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(const GatherArgs a) {
     if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 1, b, j, found)) return;
     int q0, n;
     rows_of(a.bt, b, q0, n);
-    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    const int slot = slot_of(a.bt, b);
     const int rows = min(n - j * kBlock, kBlock);  // rows of this block that the caller wants
     if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
     const int per_page = a.pt.page_tokens / kBlock;
-    const int there = min(max(a.pt.lens[slot], 0) - j * kBlock, kBlock);  // tokens of it that the sequence has
+    const int there = min(max(scalar_load(a.pt.lens + slot), 0) - j * kBlock, kBlock);  // tokens of it that the sequence has
     const bool beyond = (int64_t)j * kBlock >= (int64_t)a.pt.width * a.pt.page_tokens;
     int in_page;
     const int page = beyond ? -1 : page_of(a.pt, slot, j, per_page, in_page);
     const size_t blk = page < 0 ? 0 : ((size_t)page * Hkv + h) * per_page + in_page;
     const uint8_t *codes = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
-    const float scale = page < 0 ? __builtin_nanf("") : (is_v ? a.c.v_scale : a.c.k_scale)[blk];
+    const float scale = page < 0 ? __builtin_nanf("") : scalar_load((is_v ? a.c.v_scale : a.c.k_scale) + blk);
     uint16_t *out = (is_v ? a.v : a.k) + ((int64_t)(q0 + j * kBlock) * Hkv + h) * D;
     const int64_t st = (int64_t)Hkv * D;
     const auto value = [&](uint32_t w, int i) -> float {

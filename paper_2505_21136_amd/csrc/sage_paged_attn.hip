@@ -100,7 +100,7 @@ struct Mfma<32> {
 
 // D: head dimension; M: rows per wavefront, 16 or 32.
 template <int D, bool BF16, bool E4M3, int M>
-__global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int NL = D / 16;       // loads of 16 bytes a lane for a block of K, and of V
     constexpr int R = M * M / 64;    // registers of an accumulator tile
@@ -116,10 +116,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
     if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
     int q0, n;
     rows_of(a.bt, b, q0, n);
-    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    const int slot = slot_of(a.bt, b);
+    const int tiles = (n * a.group + ROWS - 1) / ROWS;
+    if (tile >= tiles || slot < 0 || slot >= a.pt.slots) return;
+    tile = tiles - 1 - tile;  // (causal: the tiles with the most keys first)
     const int rows = min(n * a.group - tile * ROWS, ROWS);  // of this workgroup
-    if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
-    const int cap = a.pt.width * a.pt.page_tokens, true_len = max(a.pt.lens[slot], 0), len = min(true_len, cap);
+    const int cap = a.pt.width * a.pt.page_tokens, true_len = max(scalar_load(a.pt.lens + slot), 0), len = min(true_len, cap);
 
     // ---- this wavefront's rows and blocks ----
     const int RW = rows > 2 * M ? 4 : rows > M ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
@@ -137,12 +139,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
     float row_scale;
     const int ri0 = min(first + min(lq, max(mine, 1) - 1), n * a.group - 1);
     const int lim = last_key(ri0);
+    uint4 qx[QS];
     {
         const int tok = ri0 / a.group, hq = kvh * a.group + ri0 % a.group;
         const uint16_t *p = a.q + (int64_t)(q0 + tok) * a.q_st.t + hq * a.q_st.h + 16 * g;
-        uint4 x[QS];
 #pragma unroll
-        for (int i = 0; i < QS; ++i) x[i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
+        for (int i = 0; i < QS; ++i) qx[i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
+    }
+    const auto convert_q = [&]() {
         float s = 1.0f;
         row_scale = a.scale;
         if constexpr (BF16) {
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
                 float f[8];
-                unpack8<true>(x[i], f);
+                unpack8<true>(qx[i], f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
             }
@@ -164,27 +168,31 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
         for (int i = 0; i < QS; ++i) {
             if constexpr (BF16) {
                 float f[8];
-                unpack8<true>(x[i], f);
+                unpack8<true>(qx[i], f);
                 const uint4 w = make_uint4(pack_half(f[0] * s, f[1] * s), pack_half(f[2] * s, f[3] * s),
                                            pack_half(f[4] * s, f[5] * s), pack_half(f[6] * s, f[7] * s));
                 qh[i] = __builtin_bit_cast(v8h, w);
             } else {
-                qh[i] = __builtin_bit_cast(v8h, x[i]);
+                qh[i] = __builtin_bit_cast(v8h, qx[i]);
             }
         }
-    }
+    };
     float m = -INFINITY, l = 0.0f, vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
     acc_t o[OT];
 #pragma unroll
     for (int i = 0; i < OT; ++i) o[i] = acc_t{};
 
     // ---- the keys, block by block ----
-    const int per_page = a.pt.page_tokens / kBlock;
-    const auto block_at = [&](int j, size_t &blk) {  // false: the table has no page there
-        int in_page;
-        const int page = page_of(a.pt, slot, j, per_page, in_page);
-        blk = ((size_t)max(page, 0) * a.Hkv + kvh) * per_page + (page < 0 ? 0 : in_page);
-        return page >= 0;
+    // the place of the block that is fetched next: page number `at_page` of the slot, block `at_block` of it; a step of KW blocks is
+    // `step_pages` pages and `step_blocks` blocks (no division in the loop)
+    const int per_page = a.pt.page_tokens / kBlock, step_pages = KW / per_page, step_blocks = KW - step_pages * per_page;
+    int at_page = (jb + kg) / per_page, at_block = jb + kg - at_page * per_page;
+    const int32_t *table = a.pt.table + (size_t)slot * a.pt.width;
+    const auto block_here = [&](size_t &blk) {  // false: the table has no page there
+        const int page = at_page < a.pt.width ? scalar_load(table + at_page) : -1;
+        const bool there = page >= 0 && page < a.pt.n_pages;
+        blk = ((size_t)(there ? page : 0) * a.Hkv + kvh) * per_page + (there ? at_block : 0);
+        return there;
     };
     // M = 16: load i is the i-th KB of the block.  M = 32: a lane takes its place in KB pairs, halves of 512 bytes at a time: of K key tile
     // i / (2 D/64), channels 64 (i / 2 % (D/64)) + 32 (i & 1) + 16 g ..; of V channels 32 (i / 2) .., tokens 16 w + 8 (i & 1) + 4 g ..
@@ -206,8 +214,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
     size_t blk = 0;
     float ks = 0.0f, vs = 0.0f;
     const auto scales_of = [&](bool there) {
-        ks = there ? a.k_scale[blk] : __builtin_nanf("");
-        vs = there ? a.v_scale[blk] : __builtin_nanf("");
+        ks = there ? scalar_load(a.k_scale + blk) : __builtin_nanf("");
+        vs = there ? scalar_load(a.v_scale + blk) : __builtin_nanf("");
     };
 
     acc_t s[KT];
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
         const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
         const float alpha = __builtin_amdgcn_exp2f(m - base);
         // V's scale goes into the exponent (a block of zeros: any will do)
-        const float vnew = fmaxf(vref, vs), back = vnew > 0.0f ? vref * __builtin_amdgcn_rcpf(vnew) : 0.0f;
+        const float vnew = fmaxf(vref, vs), back = vnew > vref ? vref * __builtin_amdgcn_rcpf(vnew) : 1.0f;
         const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
         const float shift = (vs == vs ? lr : vs) - base;
         float sum = 0.0f;
@@ -256,17 +264,22 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void paged_rows_kernel(const Pa
         return alpha * back;  // what o is to be multiplied by
     };
 
+    // (the table is asked before the length is known, and the first block is on its way before Q is waited for)
+    const bool there0 = block_here(blk);
     jb += kg;
     if (jb < je) {
-        const bool there = block_at(jb, blk);
         load_k(blk);
         load_v(blk);
-        scales_of(there);
+        scales_of(there0);
     }
+    convert_q();
     for (int j = jb; j < je; j += KW) {
-        const int next = j + KW < je ? j + KW : j;  // (the last one loads its own block again: no branch around the loads)
+        if (j + KW < je) {  // (the last one fetches its own block again: no branch around the loads)
+            at_page += step_pages, at_block += step_blocks;
+            if (at_block >= per_page) at_block -= per_page, ++at_page;
+        }
         size_t nblk;
-        const bool there = block_at(next, nblk);
+        const bool there = block_here(nblk);
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -369,7 +382,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a) {
     if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
     int q0, n;
     rows_of(a.bt, b, q0, n);
-    const int slot = a.bt.slots ? a.bt.slots[b] : b;
+    const int slot = slot_of(a.bt, b);
     const int rows = min(n * a.group - tile * ROWS, ROWS);
     if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
     const int r = threadIdx.x / EACH, e = threadIdx.x % EACH;
