@@ -30,42 +30,44 @@ __device__ __forceinline__ float scalar_load(const float *p) {
     return *(const __attribute__((address_space(4))) float *)(uint64_t)p;
 }
 
-// Sequence b's rows, within 0 .. T whatever q_start holds.
-__device__ __forceinline__ void rows_of(const Batch &bt, int b, int &q0, int &n) {
-    if (bt.q_start) {
-        q0 = min(max(scalar_load(bt.q_start + b), 0), bt.T);
-        n = max(min(max(scalar_load(bt.q_start + b + 1), 0), bt.T) - q0, 0);
-    } else {
-        q0 = b * bt.n, n = bt.n;
-    }
-}
+// What a workgroup works on: rows q0 .. q0 + n - 1 of the call, which belong to `slot` with `len` tokens (as the table says, any number), and
+// which of their tiles.
+struct Work {
+    int q0, n, slot, len, tile;
+};
 
 // Tile `x` of a grid over all sequences' rows in tiles of `rows`, `per` of them to a token (a token's `group` query heads: group
-// rows): which sequence and which of its tiles.  Uniform batches: by division.  Ragged ones: sequence b owns the tiles from
-// floor(q_start[b] * per / rows) + extra * b on -- as many as it can need, since ceil(n p / r) <= floor((a + n) p / r) - floor(a p / r) + 1
+// rows).  Uniform batches: by division.  Ragged ones: sequence b owns the tiles from
+// floor(q_start[b] * per / rows) + b on -- as many as it can need, since ceil(n p / r) <= floor((a + n) p / r) - floor(a p / r) + 1
 // -- and the threads of the workgroup look at all of them at once (one round of loads for up to blockDim.x sequences, where a search by
-// halves would wait for memory log2(B) times).  extra = 1, or 2 where a sequence's tiles begin in the middle of one.  Returns false
-// for a tile that nobody needs.  Has a barrier.
-__device__ __forceinline__ bool locate(const Batch &bt, int x, int rows, int per, int extra, int &b, int &tile, int *shared) {
+// halves would wait for memory log2(B) times); the one that finds it fetches the length too.  Returns false for a tile that nobody needs
+// and for padding.  Has a barrier; `shared` holds five numbers.
+__device__ __forceinline__ bool locate(const Batch &bt, const sage_page_table &pt, int x, int rows, int per, Work &w, int *shared) {
     if (!bt.q_start) {
-        const int tiles = (int)(((int64_t)bt.n * per + rows - 1) / rows) + extra - 1;
-        b = x / tiles, tile = x % tiles;
-        return b < bt.B;
+        const int tiles = (int)(((int64_t)bt.n * per + rows - 1) / rows), b = x / tiles;
+        if (b >= bt.B) return false;
+        w.tile = x - b * tiles, w.q0 = b * bt.n, w.n = bt.n;
+        w.slot = bt.slots ? scalar_load(bt.slots + b) : b;
+        if (w.slot < 0 || w.slot >= pt.slots) return false;
+        w.len = scalar_load(pt.lens + w.slot);
+        return true;
     }
-    if (threadIdx.x == 0) shared[0] = -1;
+    if (threadIdx.x == 0) shared[2] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < bt.B; i += blockDim.x) {
-        const int64_t q0 = min(max(bt.q_start[i], 0), bt.T), q1 = min(max(bt.q_start[i + 1], 0), bt.T);
-        const int first = (int)(q0 * per / rows) + extra * i, next = (int)(q1 * per / rows) + extra * (i + 1);
-        if (x >= first && x < next) shared[0] = i, shared[1] = x - first;
+        const int q0 = min(max(bt.q_start[i], 0), bt.T), q1 = min(max(bt.q_start[i + 1], 0), bt.T);
+        const int slot = bt.slots ? bt.slots[i] : i;
+        const int first = (int)((int64_t)q0 * per / rows) + i, next = (int)((int64_t)q1 * per / rows) + i + 1;
+        if (x >= first && x < next && q1 > q0 && slot >= 0 && slot < pt.slots) {
+            const int len = pt.lens[slot];
+            shared[0] = x - first, shared[1] = q0, shared[2] = q1 - q0, shared[3] = slot, shared[4] = len;
+        }
     }
     __syncthreads();
-    b = __builtin_amdgcn_readfirstlane(shared[0]), tile = __builtin_amdgcn_readfirstlane(shared[1]);
-    return b >= 0;
+    const auto uniform = [&](int i) { return __builtin_amdgcn_readfirstlane(shared[i]); };
+    w.tile = uniform(0), w.q0 = uniform(1), w.n = uniform(2), w.slot = uniform(3), w.len = uniform(4);
+    return w.n > 0;
 }
-
-// Sequence b's slot.
-__device__ __forceinline__ int slot_of(const Batch &bt, int b) { return bt.slots ? scalar_load(bt.slots + b) : b; }
 
 // The page that holds block j (of 64 tokens) of a slot, -1 where the table has none.
 __device__ __forceinline__ int page_of(const sage_page_table &pt, int slot, int j, int per_page, int &in_page) {

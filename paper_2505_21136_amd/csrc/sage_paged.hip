@@ -51,174 +51,191 @@ struct AppendArgs {
 };
 
 // One workgroup of 2 D threads quantises one block of 64 tokens of one head, of K (blockIdx.y even) or V, whatever part of it is new: tokens
-// of earlier calls come from the slot's tail.
+// of earlier calls come from the slot's tail.  The last workgroup of a sequence takes the block behind its own too, if the tokens reach
+// it (n tokens touch ceil(n / 64) blocks or one more).
 //   K: a thread takes 16 channels of two tokens (the 8 pairs that rotate together), which are 16 neighbouring bytes of the cache,
 //      or two runs of 8.
 //   V: a thread takes 2 channels of the 16 tokens whose codes are neighbours in the cache, 16 bytes per channel; a wavefront's loads are
 //      whole rows of 256 bytes.
+// Values stay in registers in 16 bits and are widened twice, for the maximum and for the codes: 80 registers, six wavefronts per SIMD, which
+// the chain table -- tokens -- maximum -- codes needs to keep memory busy.
 // The tail's two halves hold the tokens of the sequence's last two blocks.  The half that the first touched block stands in is
 // written by that block's workgroup alone, after it has read it (a barrier in between); the other half by the next block's.  So no
 // workgroup writes what another reads.
-template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(2 * D) void append_kernel(const AppendArgs a, const sage_rope_plan plan) {
-    __shared__ int found[2];
-    __shared__ float red[2][4];
+template <int D, bool BF16, bool E4M3, bool is_v>
+__device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_rope_plan &plan, const Work &wk, int h, float (&red)[2][2][4]) {
     constexpr int WAVES = 2 * D / 64;
-    const int Hkv = a.c.Hkv, h = (int)(blockIdx.y >> 1);
-    const bool is_v = blockIdx.y & 1;
-    int b, x;
-    if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 2, b, x, found)) return;
-    int q0, n;
-    rows_of(a.bt, b, q0, n);
-    const int slot = slot_of(a.bt, b);
-    if (n == 0 || slot < 0 || slot >= a.pt.slots) return;
-    const int len = min(scalar_load(a.pt.lens + slot), a.pt.width * a.pt.page_tokens);
+    const int Hkv = a.c.Hkv;
+    const int q0 = wk.q0, n = wk.n, slot = wk.slot, len = min(wk.len, a.pt.width * a.pt.page_tokens);
     const int start = max(len - n, 0);  // first new token; row q0 + p - (len - n) is token p
     const int row0 = q0 - (len - n);
-    const int j0 = start / kBlock, jl = (len - 1) / kBlock, j = j0 + x;
-    if (len <= 0 || j > jl) return;
-    const uint16_t *src = is_v ? a.v : a.k;
+    const int j0 = start / kBlock, jl = (len - 1) / kBlock;
+    if (len <= 0 || j0 + wk.tile > jl) return;
+    const int x_end = (wk.tile + 1) * kBlock >= n ? jl - j0 : wk.tile;  // the last workgroup goes on to the last block
     const TokenStrides st = is_v ? a.v_st : a.k_st;
-    uint16_t *tail = static_cast<uint16_t *>(is_v ? a.c.v_tail : a.c.k_tail) + ((size_t)slot * Hkv + h) * kTail * D;
-    const uint16_t *head = src + h * st.h;
     const int tid = threadIdx.x;
-    // the block whose tokens this workgroup puts into the tail: the last or the last but one, of its parity
-    const int keep = (x == 0 || x == 1) ? ((jl ^ j) & 1 ? jl - 1 : jl) : -1;
 
-    // K's values, 8 pairs (or 16 channels) of token p of the block jj, rotated and rounded, as 16-bit values
-    const int item = tid % (D / 16), half = plan.rot / 2;
+    // K: 8 pairs (or 16 channels) of a token
+    const int item = tid % (D / 16), half = plan.rot / 2, r0 = tid / (D / 16);
     const bool turns = a.rope && 16 * item < plan.rot, halves = turns && plan.layout == SAGE_ROPE_HALF;
     const int c0 = halves ? 8 * item : 16 * item, c1 = halves ? half + 8 * item : 16 * item + 8;
-    const auto load_k = [&](int p, uint4 (&w)[2]) {
-        w[0] = w[1] = make_uint4(0, 0, 0, 0);
-        if (p >= len) return;
-        const bool fresh = p >= start;
-        const uint16_t *r = fresh ? head + (int64_t)(row0 + p) * st.t : tail + (size_t)(p % kTail) * D;
-        w[0] = *reinterpret_cast<const uint4 *>(r + c0);
-        w[1] = *reinterpret_cast<const uint4 *>(r + c1);
-        if (fresh && turns) {
-            float cs[8], sn[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                rope_angle(p, plan.turns[8 * item + i], cs[i], sn[i]);
-                cs[i] *= plan.magnitude;
-                sn[i] *= plan.magnitude;
-            }
-            rope_turn<BF16>(halves, cs, sn, w[0], w[1]);
-        }
-    };
-    // V's: channels 2 cp, 2 cp + 1 of the block's tokens 32 u + 16 hh + 4 g + i, one 32-bit word a token
+    // V: channels 2 cp, 2 cp + 1 of tokens 32 u + 16 hh + 4 g + i
     const int g = tid / (D / 2), cp = tid % (D / 2);
     const auto v_token = [&](int i) { return 32 * (i >> 3) + 16 * (i >> 2 & 1) + 4 * g + (i & 3); };
-    const auto load_v = [&](int p) -> uint32_t {
-        if (p >= len) return 0;
-        const uint16_t *r = p >= start ? head + (int64_t)(row0 + p) * st.t : tail + (size_t)(p % kTail) * D;
-        return *reinterpret_cast<const uint32_t *>(r + 2 * cp);
-    };
-    const int p0 = j * kBlock, r0 = tid / (D / 16);
 
-    // ---- the block's values, its largest one, and whether all are finite ----
-    float f[4][8];  // K: token r0 (two runs of 8), token r0 + 32 (two); V: [channel][token] in two halves of 8
+    uint16_t *tail = static_cast<uint16_t *>(is_v ? a.c.v_tail : a.c.k_tail) + ((size_t)slot * Hkv + h) * kTail * D;
+    const uint16_t *head = (is_v ? a.v : a.k) + h * st.h;
+    const auto row_of = [&](int p) {
+        return p >= start ? head + (int64_t)(row0 + p) * st.t : tail + (size_t)(p % kTail) * D;
+    };
     uint4 kw[2][2];
     uint32_t vw[16];
-    if (!is_v) {
-        float sh[2][8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sh[0][i] = a.c.k_shift ? a.c.k_shift[h * D + c0 + i] : 0.0f;
-            sh[1][i] = a.c.k_shift ? a.c.k_shift[h * D + c1 + i] : 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int p = p0 + r0 + 32 * e;
-            load_k(p, kw[e]);
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                unpack8<BF16>(kw[e][o], f[2 * e + o]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[2 * e + o][i] = p < len ? f[2 * e + o][i] - sh[o][i] : 0.0f;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) vw[i] = load_v(p0 + v_token(i));
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            f[i >> 3][i & 7] = to_f32<BF16>(vw[i] & 0xffffu);
-            f[2 + (i >> 3)][i & 7] = to_f32<BF16>(vw[i] >> 16);
-        }
-    }
-    float amax = 0.0f, odd = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            amax = fmaxf(amax, fabsf(f[e][i]));
-            if (!(fabsf(f[e][i]) <= FLT_MAX)) odd = 1.0f;
-        }
-    amax = wave_max(amax);
-    odd = wave_max(odd);
-    if ((tid & 63) == 0) red[0][tid >> 6] = amax, red[1][tid >> 6] = odd;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) amax = fmaxf(amax, red[0][w]), odd = fmaxf(odd, red[1][w]);
-    const bool bad = odd != 0.0f;
-    float scale, factor;
-    block_scale<E4M3>(amax, bad, scale, factor);
-    if (bad) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[e][i] = 0.0f;
-    }
-
-    // ---- codes and scale ----
-    int in_page;
-    const int per_page = a.pt.page_tokens / kBlock, page = page_of(a.pt, slot, j, per_page, in_page);
-    if (page >= 0) {
-        const size_t blk = ((size_t)page * Hkv + h) * per_page + in_page;
-        uint8_t *out = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
-        if (tid == 0) (is_v ? a.c.v_scale : a.c.k_scale)[blk] = scale;
-        if (!is_v) {
+    // the block's values in 16 bits, zeros behind the last token; K's new ones rotated and rounded
+    const auto load = [&](int p0) {
+        if constexpr (!is_v) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int r = r0 + 32 * e;
-                const uint2 lo = cache_codes<E4M3>(f[2 * e], factor), hi = cache_codes<E4M3>(f[2 * e + 1], factor);
-                const auto at = [&](int ch) { return (((r >> 4) * (D / 64) + (ch >> 6)) * 64 + (ch >> 4 & 3) * 16 + (r & 15)) * 16 + (ch & 15); };
-                *reinterpret_cast<uint2 *>(out + at(c0)) = lo;
-                *reinterpret_cast<uint2 *>(out + at(c1)) = hi;
+                const uint16_t *r = row_of(min(p0 + r0 + 32 * e, len - 1));  // (no branch around the loads; see the end of this function)
+                kw[e][0] = *reinterpret_cast<const uint4 *>(r + c0);
+                kw[e][1] = *reinterpret_cast<const uint4 *>(r + c1);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int p = p0 + r0 + 32 * e;
+                if (!turns || p < start || p >= len) continue;
+                float cs[8], sn[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    rope_angle(p, plan.turns[8 * item + i], cs[i], sn[i]);
+                    cs[i] *= plan.magnitude;
+                    sn[i] *= plan.magnitude;
+                }
+                rope_turn<BF16>(halves, cs, sn, kw[e][0], kw[e][1]);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (p0 + r0 + 32 * e >= len) kw[e][0] = kw[e][1] = make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) vw[i] = *reinterpret_cast<const uint32_t *>(row_of(min(p0 + v_token(i), len - 1)) + 2 * cp);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) vw[i] = p0 + v_token(i) < len ? vw[i] : 0;
+        }
+    };
+    // eight values in binary32: K: run o of token e (2 e + o); V: channel ch's tokens 8 u .. (2 ch + u)
+    const auto values = [&](int k, int p0, float (&f)[8]) {
+        if constexpr (!is_v) {
+            const int e = k >> 1, o = k & 1;
+            unpack8<BF16>(kw[e][o], f);
+            if (a.c.k_shift) {
+                const float4 *sh = reinterpret_cast<const float4 *>(a.c.k_shift + h * D + (o ? c1 : c0));
+                const float4 s0 = sh[0], s1 = sh[1];
+                const bool in = p0 + r0 + 32 * e < len;
+                const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = in ? f[i] - s[i] : 0.0f;
             }
         } else {
 #pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-                const uint2 lo = cache_codes<E4M3>(f[2 * ch], factor), hi = cache_codes<E4M3>(f[2 * ch + 1], factor);
-                const int c = 2 * cp + ch;
-                *reinterpret_cast<uint4 *>(out + ((c >> 4) * 64 + 16 * g + (c & 15)) * 16) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            for (int i = 0; i < 8; ++i) f[i] = to_f32<BF16>(k >> 1 ? vw[8 * (k & 1) + i] >> 16 : vw[8 * (k & 1) + i] & 0xffffu);
+        }
+    };
+
+    for (int x = wk.tile; x <= x_end; ++x) {
+        const int j = j0 + x, p0 = j * kBlock;
+        int in_page;
+        const int per_page = a.pt.page_tokens / kBlock, page = page_of(a.pt, slot, j, per_page, in_page);
+        load(p0);
+        // ---- the largest value, and whether all are finite ----
+        float amax = 0.0f, odd = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float f[8];
+            values(k, p0, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                amax = fmaxf(amax, fabsf(f[i]));
+                if (!(fabsf(f[i]) <= FLT_MAX)) odd = 1.0f;
+            }
+        }
+        // (what was widened is let go)
+        if constexpr (!is_v) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(kw[e >> 1][e & 1].x), "+v"(kw[e >> 1][e & 1].y), "+v"(kw[e >> 1][e & 1].z), "+v"(kw[e >> 1][e & 1].w));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(vw[i]));
+        }
+        amax = wave_max(amax);
+        odd = wave_max(odd);
+        if ((tid & 63) == 0) red[x & 1][0][tid >> 6] = amax, red[x & 1][1][tid >> 6] = odd;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) amax = fmaxf(amax, red[x & 1][0][w]), odd = fmaxf(odd, red[x & 1][1][w]);
+        float scale, factor;
+        block_scale<E4M3>(amax, odd != 0.0f, scale, factor);
+
+        // ---- codes and scale ----
+        if (page >= 0) {
+            const size_t blk = ((size_t)page * Hkv + h) * per_page + in_page;
+            uint8_t *out = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
+            if (tid == 0) (is_v ? a.c.v_scale : a.c.k_scale)[blk] = scale;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                uint2 w[2];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    float f[8];
+                    values(2 * e + o, p0, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = odd != 0.0f ? 0.0f : f[i];
+                    w[o] = cache_codes<E4M3>(f, factor);
+                }
+                if constexpr (!is_v) {
+                    const int r = r0 + 32 * e;
+                    const auto at = [&](int ch) { return (((r >> 4) * (D / 64) + (ch >> 6)) * 64 + (ch >> 4 & 3) * 16 + (r & 15)) * 16 + (ch & 15); };
+                    *reinterpret_cast<uint2 *>(out + at(c0)) = w[0];
+                    *reinterpret_cast<uint2 *>(out + at(c1)) = w[1];
+                } else {
+                    const int c = 2 * cp + e;
+                    *reinterpret_cast<uint4 *>(out + ((c >> 4) * 64 + 16 * g + (c & 15)) * 16) = make_uint4(w[0].x, w[0].y, w[1].x, w[1].y);
+                }
+            }
+        }
+
+        // ---- the tail: the last block or the last but one, of this block's parity ----
+        const int keep = x > 1 ? -1 : (jl ^ j) & 1 ? jl - 1 : jl;
+        if (keep < j) continue;
+        const int k0 = keep * kBlock;
+        if (keep != j) load(k0);
+        if constexpr (!is_v) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int p = k0 + r0 + 32 * e;
+                if (p < start || p >= len) continue;
+                *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c0) = kw[e][0];
+                *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c1) = kw[e][1];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int p = k0 + v_token(i);
+                if (p < start || p >= len) continue;
+                *reinterpret_cast<uint32_t *>(tail + (size_t)(p % kTail) * D + 2 * cp) = vw[i];
             }
         }
     }
+}
 
-    // ---- the tail ----
-    if (keep < j) return;
-    const int k0 = keep * kBlock;
-    if (!is_v) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int p = k0 + r0 + 32 * e;
-            if (p < start || p >= len) continue;
-            if (keep != j) load_k(p, kw[e]);
-            *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c0) = kw[e][0];
-            *reinterpret_cast<uint4 *>(tail + (size_t)(p % kTail) * D + c1) = kw[e][1];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int p = k0 + v_token(i);
-            if (p < start || p >= len) continue;
-            if (keep != j) vw[i] = load_v(p);
-            *reinterpret_cast<uint32_t *>(tail + (size_t)(p % kTail) * D + 2 * cp) = vw[i];
-        }
-    }
+template <int D, bool BF16, bool E4M3>
+__global__ __launch_bounds__(2 * D, 6) void append_kernel(const AppendArgs a, const sage_rope_plan plan) {
+    __shared__ int found[5];
+    __shared__ float red[2][2][4];
+    Work wk;
+    if (!locate(a.bt, a.pt, (int)blockIdx.x, kBlock, 1, wk, found)) return;
+    const int h = (int)(blockIdx.y >> 1);
+    if (blockIdx.y & 1) append_blocks<D, BF16, E4M3, true>(a, plan, wk, h, red);
+    else append_blocks<D, BF16, E4M3, false>(a, plan, wk, h, red);
 }
 
 struct GatherArgs {
@@ -232,18 +249,16 @@ struct GatherArgs {
 // lanes take neighbouring channels of a token: the rows that are written are twice the bytes of the codes that are read.
 template <int D, bool BF16, bool E4M3>
 __global__ __launch_bounds__(2 * D) void gather_kernel(const GatherArgs a) {
-    __shared__ int found[2];
+    __shared__ int found[5];
     const int Hkv = a.c.Hkv, h = (int)(blockIdx.y >> 1), tid = threadIdx.x;
     const bool is_v = blockIdx.y & 1;
-    int b, j;
-    if (!locate(a.bt, (int)blockIdx.x, kBlock, 1, 1, b, j, found)) return;
-    int q0, n;
-    rows_of(a.bt, b, q0, n);
-    const int slot = slot_of(a.bt, b);
-    const int rows = min(n - j * kBlock, kBlock);  // rows of this block that the caller wants
-    if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
+    Work wk;
+    if (!locate(a.bt, a.pt, (int)blockIdx.x, kBlock, 1, wk, found)) return;
+    const int q0 = wk.q0, j = wk.tile, slot = wk.slot;
+    const int rows = min(wk.n - j * kBlock, kBlock);  // rows of this block that the caller wants
+    if (rows <= 0) return;
     const int per_page = a.pt.page_tokens / kBlock;
-    const int there = min(max(scalar_load(a.pt.lens + slot), 0) - j * kBlock, kBlock);  // tokens of it that the sequence has
+    const int there = min(max(wk.len, 0) - j * kBlock, kBlock);  // tokens of it that the sequence has
     const bool beyond = (int64_t)j * kBlock >= (int64_t)a.pt.width * a.pt.page_tokens;
     int in_page;
     const int page = beyond ? -1 : page_of(a.pt, slot, j, per_page, in_page);
@@ -261,9 +276,14 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(const GatherArgs a) {
     };
     if (!is_v) {
         const int item = tid % (D / 16);
-        float sh[16];
+        float sh[16] = {};
+        if (a.c.k_shift) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sh[i] = a.c.k_shift ? a.c.k_shift[h * D + 16 * item + i] : 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                const float4 s = reinterpret_cast<const float4 *>(a.c.k_shift + h * D + 16 * item)[i];
+                sh[4 * i] = s.x, sh[4 * i + 1] = s.y, sh[4 * i + 2] = s.z, sh[4 * i + 3] = s.w;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = tid / (D / 16) + 32 * e;
@@ -339,7 +359,7 @@ hipError_t launch_paged_append(const sage_page_table &pt, const sage_cache &c, c
     AppendArgs a{pt, c, static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), k_st, v_st, bt, rope != nullptr};
     static const sage_rope_plan none = {};
     const sage_rope_plan &plan = rope ? *rope : none;
-    const int64_t tiles = bt.q_start ? bt.T / kBlock + 2 * (int64_t)bt.B : (int64_t)bt.B * (cdiv(bt.n, kBlock) + 1);
+    const int64_t tiles = bt.q_start ? bt.T / kBlock + (int64_t)bt.B : (int64_t)bt.B * cdiv(bt.n, kBlock);
     const dim3 grid((unsigned)tiles, 2 * c.Hkv), block(2 * c.d);
     const bool bf16 = c.dt == SAGE_BF16, e4m3 = c.fmt == SAGE_CACHE_E4M3;
     if (c.d == 128)

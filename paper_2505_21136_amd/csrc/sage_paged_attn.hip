@@ -107,21 +107,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     constexpr int KT = 64 / M, OT = D / M, NP = KT * R, ROWS = M * kAttnWaves, LD = D + 4;
     constexpr int QS = D / (512 / M); // matrix instructions that a key tile's scores take (8 channels a lane each)
     typedef typename Mfma<M>::acc acc_t;
-    __shared__ int found[2];
+    __shared__ int found[5];
     __shared__ __attribute__((aligned(16))) float acc_lds[kAttnWaves * M * LD];
     __shared__ float2 ml_lds[kAttnWaves * M];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane % M, g = lane / M;
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv, split = blockIdx.y;
-    int b, tile;
-    if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
-    int q0, n;
-    rows_of(a.bt, b, q0, n);
-    const int slot = slot_of(a.bt, b);
-    const int tiles = (n * a.group + ROWS - 1) / ROWS;
-    if (tile >= tiles || slot < 0 || slot >= a.pt.slots) return;
-    tile = tiles - 1 - tile;  // (causal: the tiles with the most keys first)
+    Work wk;
+    if (!locate(a.bt, a.pt, slot_x, ROWS, a.group, wk, found)) return;
+    const int q0 = wk.q0, n = wk.n, slot = wk.slot, tiles = (n * a.group + ROWS - 1) / ROWS;
+    if (wk.tile >= tiles) return;
+    const int tile = tiles - 1 - wk.tile;  // (causal: the tiles with the most keys first)
     const int rows = min(n * a.group - tile * ROWS, ROWS);  // of this workgroup
-    const int cap = a.pt.width * a.pt.page_tokens, true_len = max(scalar_load(a.pt.lens + slot), 0), len = min(true_len, cap);
+    const int cap = a.pt.width * a.pt.page_tokens, true_len = max(wk.len, 0), len = min(true_len, cap);
 
     // ---- this wavefront's rows and blocks ----
     const int RW = rows > 2 * M ? 4 : rows > M ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
@@ -370,65 +367,89 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
 }
 
 // The ranges of a row combined as partial softmax sums.  A workgroup per 1024 / D packed rows of a K/V head, a thread per four channels of a row.
-// Bound by latency with few rows: the ranges' weights are computed by all threads at once and meet in LDS, then eight ranges' sums are
-// in flight per thread.  Ranges that the row sees nothing of have no sums; what lies in their place is not used.
-template <int D, bool BF16>
+// Bound by latency with few rows: up to FEW ranges a thread fetches all of them at once, weights and sums; beyond, the weights are
+// computed by all threads of the row and meet in LDS, and eight ranges' sums are in flight per thread.  Ranges that the row sees nothing
+// of have no sums; what lies in their place is not used.
+template <int D, bool BF16, int FEW>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a) {
     constexpr int ROWS = 1024 / D, EACH = 256 / ROWS, CHUNK = 256;  // EACH: threads per row
-    __shared__ int found[2];
-    __shared__ float weight[ROWS][CHUNK];
+    __shared__ int found[5];
+    __shared__ float weight[FEW ? 1 : ROWS][CHUNK];
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv;
-    int b, tile;
-    if (!locate(a.bt, slot_x, ROWS, a.group, 1, b, tile, found)) return;
-    int q0, n;
-    rows_of(a.bt, b, q0, n);
-    const int slot = slot_of(a.bt, b);
-    const int rows = min(n * a.group - tile * ROWS, ROWS);
-    if (rows <= 0 || slot < 0 || slot >= a.pt.slots) return;
+    Work wk;
+    if (!locate(a.bt, a.pt, slot_x, ROWS, a.group, wk, found)) return;
+    const int rows = min(wk.n * a.group - wk.tile * ROWS, ROWS);
+    if (rows <= 0) return;
     const int r = threadIdx.x / EACH, e = threadIdx.x % EACH;
-    const int ri = tile * ROWS + min(r, rows - 1), tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
+    const int ri = wk.tile * ROWS + min(r, rows - 1), tok = wk.q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
     const size_t row0 = (size_t)tok * a.Hq + hq, step = (size_t)a.bt.T * a.Hq;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
-    const auto lanes = [](float x, auto op) {  // over the row's EACH lanes
-#pragma unroll
-        for (int d = 1; d < EACH; d <<= 1) x = op(x, __shfl_xor(x, d));
-        return x;
-    };
-    float mx = -INFINITY;
-    for (int s = e; s < a.splits; s += EACH) mx = fmaxf(mx, ml[row0 + s * step].x);
-    mx = lanes(mx, [](float x, float y) { return fmaxf(x, y); });
-    const float base = mx == -INFINITY ? 0.0f : mx;
-    float sum = 0.0f;
+    const auto sums_of = [&](int s) { return *reinterpret_cast<const float4 *>(a.part_acc + (row0 + s * step) * D + 4 * e); };
+    const auto empty = [](const float2 &x) { return x.x == -INFINITY && x.y == 0.0f; };
+    float mx = -INFINITY, sum = 0.0f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < a.splits; s0 += CHUNK) {
-        const int here = min(a.splits - s0, CHUNK);
-        __syncthreads();
-        for (int s = e; s < here; s += EACH) {
-            const float2 x = ml[row0 + (s0 + s) * step];
-            const bool none = x.x == -INFINITY && x.y == 0.0f;
-            const float w = none ? 0.0f : __builtin_amdgcn_exp2f(x.x - base);
-            weight[r][s] = none ? -1.0f : w;
-            sum += w * x.y;
-        }
-        __syncthreads();
-        for (int s = 0; s < here; s += 8) {
-            float4 y[8];
-            float w[8];
+    const auto add = [&](float w, const float4 &y) { acc.x += w * y.x, acc.y += w * y.y, acc.z += w * y.z, acc.w += w * y.w; };
+    if constexpr (FEW > 0) {
+        float2 x[FEW];
+        float4 y[FEW];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int k = min(s + i, here - 1);
-                w[i] = s + i < here ? weight[r][k] : -1.0f;
-                y[i] = *reinterpret_cast<const float4 *>(a.part_acc + (row0 + (s0 + k) * step) * D + 4 * e);
-            }
+        for (int s = 0; s < FEW; ++s) {
+            x[s] = ml[row0 + min(s, a.splits - 1) * step];
+            y[s] = sums_of(min(s, a.splits - 1));
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (w[i] == -1.0f) continue;
-                acc.x += w[i] * y[i].x, acc.y += w[i] * y[i].y, acc.z += w[i] * y[i].z, acc.w += w[i] * y[i].w;
+        for (int s = 0; s < FEW; ++s) mx = fmaxf(mx, x[s].x);
+        const float base = mx == -INFINITY ? 0.0f : mx;
+#pragma unroll
+        for (int s = 0; s < FEW; ++s) {
+            if (s >= a.splits || empty(x[s])) continue;
+            const float w = __builtin_amdgcn_exp2f(x[s].x - base);
+            sum += w * x[s].y;
+            add(w, y[s]);
+        }
+    } else {
+        const auto lanes = [](float x, auto op) {  // over the row's EACH lanes
+#pragma unroll
+            for (int d = 1; d < EACH; d <<= 1) x = op(x, __shfl_xor(x, d));
+            return x;
+        };
+        for (int s = e; s < a.splits; s += EACH) mx = fmaxf(mx, ml[row0 + s * step].x);
+        mx = lanes(mx, [](float x, float y) { return fmaxf(x, y); });
+        const float base = mx == -INFINITY ? 0.0f : mx;
+        for (int s0 = 0; s0 < a.splits; s0 += CHUNK) {
+            const int here = min(a.splits - s0, CHUNK);
+            __syncthreads();
+            for (int s = e; s < here; s += EACH) {
+                const float2 x = ml[row0 + (s0 + s) * step];
+                const float w = empty(x) ? 0.0f : __builtin_amdgcn_exp2f(x.x - base);
+                weight[r][s] = empty(x) ? -1.0f : w;
+                sum += w * x.y;
+            }
+            __syncthreads();
+            for (int s = 0; s < here; s += 8) {
+                float4 y[8];
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int k = min(s + i, here - 1);
+                    w[i] = s + i < here ? weight[r][k] : -1.0f;
+                    y[i] = sums_of(s0 + k);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (w[i] != -1.0f) add(w[i], y[i]);  // (a NaN of a row's sums is none of them)
             }
         }
+        sum = lanes(sum, [](float x, float y) { return x + y; });
     }
-    sum = lanes(sum, [](float x, float y) { return x + y; });
     if (r < rows) store_row_quad<D, BF16>(a, tok, hq, 4 * e, acc, sum, false, 0);
+}
+
+template <int D, bool BF16>
+void launch_merge(dim3 grid, hipStream_t stream, const PagedArgs &a) {
+    if (a.splits <= 4) paged_merge_kernel<D, BF16, 4><<<grid, dim3(256), 0, stream>>>(a);
+    else if (a.splits <= 16) paged_merge_kernel<D, BF16, 16><<<grid, dim3(256), 0, stream>>>(a);
+    else paged_merge_kernel<D, BF16, 0><<<grid, dim3(256), 0, stream>>>(a);
 }
 
 template <int D, bool BF16, bool E4M3>
@@ -451,10 +472,12 @@ int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
     const int group = Hq / Hkv, rows = kAttnWaves * wave_rows(T, B, group);
     const int64_t tiles = ((int64_t)T * group + rows * (int64_t)B - 1) / (rows * (int64_t)B);  // of a sequence, at the mean
     const int64_t workgroups = tiles * B * Hkv;
-    // three workgroups per CU, ranges of at least four blocks
-    const int64_t ranges = std::max<int64_t>(1, 3 * kCUs / workgroups);
     const int64_t blocks = cdiv(max_len, kBlock);
-    return (int)std::max<int64_t>(4, (blocks + ranges - 1) / ranges) * kBlock;
+    // Few workgroups: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than their
+    // wavefronts hide.  Many: up to four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least.
+    const int64_t ranges = workgroups < kCUs ? std::min((kCUs + workgroups / 2) / workgroups, std::max<int64_t>(1, blocks / 4))
+                                             : std::min(std::max<int64_t>(1, 4 * kCUs / workgroups), std::max<int64_t>(1, blocks / 32));
+    return (int)((blocks + ranges - 1) / ranges) * kBlock;
 }
 
 PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len, int split_keys) {
@@ -490,9 +513,9 @@ hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenS
     if (e != hipSuccess || ws.splits == 1) return e;
     const dim3 mgrid((unsigned)(row_slots(bt.T, bt.B, a.group, 1024 / c.d, bt.q_start != nullptr) * c.Hkv));
     if (c.d == 128)
-        (bf16 ? paged_merge_kernel<128, true> : paged_merge_kernel<128, false>)<<<mgrid, dim3(256), 0, stream>>>(a);
+        (bf16 ? launch_merge<128, true> : launch_merge<128, false>)(mgrid, stream, a);
     else
-        (bf16 ? paged_merge_kernel<64, true> : paged_merge_kernel<64, false>)<<<mgrid, dim3(256), 0, stream>>>(a);
+        (bf16 ? launch_merge<64, true> : launch_merge<64, false>)(mgrid, stream, a);
     return hipGetLastError();
 }
 

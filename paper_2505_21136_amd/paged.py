@@ -60,13 +60,20 @@ def declare(L) -> None:
         fn.restype, fn.argtypes = result, args
 
 
+_TwoStrides = ctypes.c_int64 * 2
+
+
+def _current() -> int:
+    return _sage._current_device() if _sage._current_device is not None else torch.cuda.current_device()
+
+
 def _here(t: torch.Tensor, what: str) -> None:
     """A device tensor of the current device: the launches go to the current stream of that device."""
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0:
         raise _sage.SageError(f"{what}: libsage needs device tensors (no CPU path exists)")
-    current = _sage._current_device() if _sage._current_device is not None else torch.cuda.current_device()
-    if t.get_device() != current:
-        raise _sage.SageError(f"{what} is on device {t.get_device()}, the current device is {current}")
+    if device != _current():
+        raise _sage.SageError(f"{what} is on device {device}, the current device is {_current()}")
 
 
 def _ints(t: torch.Tensor | None, what: str, n: int | None = None) -> int | None:
@@ -83,10 +90,14 @@ def _ints(t: torch.Tensor | None, what: str, n: int | None = None) -> int | None
 
 def _rows(t: torch.Tensor, what: str):
     """[T, H, d] with contiguous channels -> the {token, head} element strides, None where contiguous."""
-    if t.dim() != 3 or t.stride(2) != 1:
+    st = t.stride()
+    if len(st) != 3 or st[2] != 1:
         raise _sage.SageError(f"{what} must be [T, H, d] with a contiguous channel dimension")
     _here(t, what)
-    return None if t.is_contiguous() else (ctypes.c_int64 * 2)(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+    if t.is_contiguous():
+        return None
+    T, H, _ = t.shape
+    return _TwoStrides(st[0] if T > 1 else 0, st[1] if H > 1 else 0)
 
 
 def rope_plan(rot: int, *, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0, trained_len: int = 0,
@@ -106,27 +117,29 @@ def sage_rope(q: torch.Tensor, positions: torch.Tensor, plan: _RopePlan, *, k: t
               out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
     """Rotary positions of q [T, Hq, d] and, in the same launch, k [T, Hkv, d] (any views with contiguous channels): -> out, or (out, k_out).
     out = q and k_out = k rotate in place."""
-    T, Hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
-    qs, Hkv = _rows(q, "q"), 0
+    qs, (T, Hq, d), Hkv = _rows(q, "q"), q.shape, 0
+    qos = ks = kos = None
     if out is None:
-        out = torch.empty((T, Hq, d), dtype=q.dtype, device=q.device)
-    if out.shape != q.shape or out.dtype != q.dtype:
-        raise _sage.SageError("out must have q's shape and dtype")
-    ks = kos = None
+        out = q.new_empty((T, Hq, d))
+    else:
+        qos = _rows(out, "out")
+        if out.shape != q.shape or out.dtype != q.dtype:
+            raise _sage.SageError("out must have q's shape and dtype")
     if k is not None:
-        Hkv, ks = k.shape[1] if k.dim() == 3 else 0, _rows(k, "k")
+        ks, Hkv = _rows(k, "k"), k.shape[1]
         if k.shape != (T, Hkv, d) or k.dtype != q.dtype:
             raise _sage.SageError("k must be [T, Hkv, d] of q's dtype")
         if k_out is None:
-            k_out = torch.empty((T, Hkv, d), dtype=q.dtype, device=q.device)
-        if k_out.shape != k.shape or k_out.dtype != k.dtype:
-            raise _sage.SageError("k_out must have k's shape and dtype")
-        kos = _rows(k_out, "k_out")
+            k_out = k.new_empty((T, Hkv, d))
+        else:
+            kos = _rows(k_out, "k_out")
+            if k_out.shape != k.shape or k_out.dtype != k.dtype:
+                raise _sage.SageError("k_out must have k's shape and dtype")
     elif k_out is not None:
         raise _sage.SageError("k_out without k")
     _sage._check(_sage.lib().sage_rope(
         q.data_ptr(), out.data_ptr(), None if k is None else k.data_ptr(), None if k is None else k_out.data_ptr(),
-        _ints(positions, "positions", T), T, Hq, Hkv, d, qs, _rows(out, "out"), ks, kos, ctypes.byref(plan), int(transposed), _sage._dt(q),
+        _ints(positions, "positions", T), T, Hq, Hkv, d, qs, qos, ks, kos, ctypes.byref(plan), int(transposed), _sage._dt(q),
         _sage._stream()))
     return out if k is None else (out, k_out)
 
@@ -228,8 +241,8 @@ def sage_paged_gather(cache: PagedCache, k_start: torch.Tensor, total: int, *, s
     """The tokens of sequence b as rows k_start[b] .. k_start[b + 1] - 1 of (k, v), [total, Hkv, d] in 16 bits; rows of no sequence are
     left unwritten."""
     B = _batch(cache, k_start, slots, "k_start")
-    k = torch.empty((total, cache.Hkv, cache.d), dtype=cache.dtype, device=cache.k.device)
-    v = torch.empty_like(k)
+    k = cache.k_tail.new_empty((total, cache.Hkv, cache.d))
+    v = cache.k_tail.new_empty((total, cache.Hkv, cache.d))
     _here(k, "the cache")
     _sage._check(_sage.lib().sage_paged_gather(cache.pages.ref, cache.ref, k.data_ptr(), v.data_ptr(), _ints(k_start, "k_start"),
                                                _ints(slots, "slots", B), B, int(total), _sage._stream()))
@@ -253,11 +266,13 @@ def sage_attn_fwd_paged(q: torch.Tensor, cache: PagedCache, *, causal: bool, max
     for T / B rows each; slots int32 [B], or None for slot b; max_len: the longest sequence expected."""
     qs = _of_cache(q, cache, "q")
     T, Hq, d = q.shape
+    os_ = None
     if out is None:
-        out = torch.empty((T, Hq, d), dtype=q.dtype, device=q.device)
-    if out.shape != q.shape:
-        raise _sage.SageError("out must have q's shape")
-    os_ = _of_cache(out, cache, "out")
+        out = q.new_empty((T, Hq, d))
+    else:
+        os_ = _of_cache(out, cache, "out")
+        if out.shape != q.shape:
+            raise _sage.SageError("out must have q's shape")
     B = _batch(cache, q_start, slots, "q_start")
     if workspace is None:
         workspace = _sage._workspace(paged_workspace_bytes(T, B, Hq, cache.Hkv, d, max_len, split_keys), q.device)
