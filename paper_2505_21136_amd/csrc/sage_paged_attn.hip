@@ -20,6 +20,7 @@ namespace {
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = SAGE_CACHE_BLOCK, kAttnWaves = 4;
 
@@ -66,17 +67,35 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {
 }
 #endif
 
-// A row's running sums on their way into the output or the workspace.
+#if defined(__HIP_DEVICE_COMPILE__)
+// The kernel's arguments, read again: what only a kernel's end needs would otherwise stay in scalar registers over the whole loop, which has
+// none to spare.
+__device__ __forceinline__ PagedArgs arguments_again() {
+    uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const __attribute__((address_space(4))) PagedArgs *)p;
+}
+#endif
+
+// Four channels of a row's output: acc / l in the output's type.
 template <int D, bool BF16>
-__device__ __forceinline__ void store_row_quad(const PagedArgs &a, int tok, int hq, int ch, const float4 &acc, float l, bool split, int s) {
-    if (split) {
-        const size_t row = ((size_t)s * a.bt.T + tok) * a.Hq + hq;
-        *reinterpret_cast<float4 *>(a.part_acc + row * D + ch) = acc;
-    } else {
-        const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // a row that saw no key is zeros, NaN stays NaN
-        uint16_t *o = a.out + tok * a.o_st.t + hq * a.o_st.h + ch;
-        *reinterpret_cast<uint2 *>(o) = make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+__device__ __forceinline__ void store_out(const PagedArgs &a, int tok, int hq, int ch, const float4 &acc, float l) {
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // a row that saw no key is zeros, NaN stays NaN
+    uint16_t *o = a.out + tok * a.o_st.t + hq * a.o_st.h + ch;
+    *reinterpret_cast<uint2 *>(o) = make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+}
+
+// The same of a range's sums, or those themselves into the workspace where there are more ranges.
+template <int D, bool BF16>
+__device__ __forceinline__ void store_sums(const PagedArgs &a, int tok, int hq, int ch, const float4 &acc, float m, float l, int split) {
+    if (a.splits == 1) {
+        store_out<D, BF16>(a, tok, hq, ch, acc, l);
+        return;
     }
+    const size_t row = ((size_t)split * a.bt.T + tok) * a.Hq + hq;
+    if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * row) = make_float2(m, l);
+    if (m == -INFINITY && l == 0.0f) return;  // (the combination does not read them)
+    *reinterpret_cast<float4 *>(a.part_acc + row * D + ch) = acc;
 }
 
 // The matrix instruction for M query rows: M = 16 (16x16x32) or 32 (32x32x16).  Of an accumulator tile a lane holds, for row lane % M, the
@@ -108,7 +127,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     constexpr int QS = D / (512 / M); // matrix instructions that a key tile's scores take (8 channels a lane each)
     typedef typename Mfma<M>::acc acc_t;
     __shared__ int found[5];
-    __shared__ __attribute__((aligned(16))) float acc_lds[kAttnWaves * M * LD];
+    constexpr bool SHARED = D == 128 && M == 32;  // four wavefronts with rows of their own share the conversion of the codes
+    constexpr int HALF = 64 * D * 2;              // bytes of a block of K, or V, in binary16
+    static_assert(!SHARED || 4 * HALF <= (int)sizeof(float) * kAttnWaves * M * LD, "two stages of K and V fit");
+    __shared__ __attribute__((aligned(1024))) float acc_lds[kAttnWaves * M * LD];
     __shared__ float2 ml_lds[kAttnWaves * M];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane % M, g = lane / M;
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv, split = blockIdx.y;
@@ -136,27 +158,26 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     float row_scale;
     const int ri0 = min(first + min(lq, max(mine, 1) - 1), n * a.group - 1);
     const int lim = last_key(ri0);
-    uint4 qx[QS];
-    {
+    const auto load_q = [&](uint4 (&qx)[QS]) {
         const int tok = ri0 / a.group, hq = kvh * a.group + ri0 % a.group;
         const uint16_t *p = a.q + (int64_t)(q0 + tok) * a.q_st.t + hq * a.q_st.h + 16 * g;
 #pragma unroll
         for (int i = 0; i < QS; ++i) qx[i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
-    }
-    const auto convert_q = [&]() {
+    };
+    const auto convert_q = [&](const uint4 (&qx)[QS]) {
         float s = 1.0f;
         row_scale = a.scale;
         if constexpr (BF16) {
             // binary16 has bfloat16's precision and more, not its range: the row is brought to 1 .. 2 by a power of two
-            float top = 0.0f;
+            // (magnitudes in order of their bits, two at a time)
+            v2u16 m2 = {0, 0};
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
-                float f[8];
-                unpack8<true>(qx[i], f);
+                const uint32_t w[4] = {qx[i].x, qx[i].y, qx[i].z, qx[i].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+                for (int e = 0; e < 4; ++e) m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(v2u16, w[e] & 0x7fff7fffu));
             }
-            top = Mfma<M>::row_max(top);
+            const float top = Mfma<M>::row_max(__builtin_bit_cast(float, (uint32_t)max(m2[0], m2[1]) << 16));
             const int ex = min(max((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127, -126), 126);
             s = __builtin_bit_cast(float, (uint32_t)(127 - ex) << 23);
             row_scale *= __builtin_bit_cast(float, (uint32_t)(127 + ex) << 23);
@@ -176,8 +197,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     };
     float m = -INFINITY, l = 0.0f, vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
     acc_t o[OT];
-#pragma unroll
-    for (int i = 0; i < OT; ++i) o[i] = acc_t{};
 
     // ---- the keys, block by block ----
     // the place of the block that is fetched next: page number `at_page` of the slot, block `at_block` of it; a step of KW blocks is
@@ -215,11 +234,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         vs = there ? scalar_load(a.v_scale + blk) : __builtin_nanf("");
     };
 
-    acc_t s[KT];
     v8h pb[NP / 8];
     // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far; MASKED: some row does not see
     // some key of the block.
-    const auto softmax = [&](auto masked_c, int key0) {
+    const auto softmax = [&](auto masked_c, acc_t (&s)[KT], int key0) {
         constexpr bool MASKED = decltype(masked_c)::value;
         const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim; };
         if constexpr (MASKED) {
@@ -261,75 +279,232 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         return alpha * back;  // what o is to be multiplied by
     };
 
-    // (the table is asked before the length is known, and the first block is on its way before Q is waited for)
-    const bool there0 = block_here(blk);
-    jb += kg;
-    if (jb < je) {
-        load_k(blk);
-        load_v(blk);
-        scales_of(there0);
-    }
-    convert_q();
-    for (int j = jb; j < je; j += KW) {
-        if (j + KW < je) {  // (the last one fetches its own block again: no branch around the loads)
-            at_page += step_pages, at_block += step_blocks;
-            if (at_block >= per_page) at_block -= per_page, ++at_page;
-        }
-        size_t nblk;
-        const bool there = block_here(nblk);
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int i = 0; i < QS / 2; ++i) {
-                const uint4 x = kx[t * (QS / 2) + i];
-                s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), qh[2 * i], i == 0 ? acc_t{} : s[t]);
-                s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), qh[2 * i + 1], s[t]);
-                if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
-            }
-        load_k(nblk);
-        const float f = j * kBlock + kBlock - 1 > lim_lo ? softmax(std::true_type{}, j * kBlock) : softmax(std::false_type{}, 0);
+    const auto advance = [&]() {
+        at_page += step_pages, at_block += step_blocks;
+        if (at_block >= per_page) at_block -= per_page, ++at_page;
+    };
+    const auto rescale = [&](float f) {  // where a maximum moved
         if (__builtin_amdgcn_ballot_w64(f != 1.0f) != 0) {
 #pragma unroll
             for (int i = 0; i < OT; ++i) o[i] *= f;
         }
-        // O^T += V^T P^T
+    };
+    const auto clear = [&]() {
 #pragma unroll
-        for (int t = 0; t < OT; ++t) {
-            if constexpr (M == 16) {
-                const uint4 x = vx[t];
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), pb[0], o[t]);
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), pb[1], o[t]);
-            } else {
-                const uint4 x = vx[2 * t], y = vx[2 * t + 1];
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, y.x), pb[0], o[t]);
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.y, y.y), pb[1], o[t]);
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, y.z), pb[2], o[t]);
-                o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.w, y.w), pb[3], o[t]);
+        for (int i = 0; i < OT; ++i) o[i] = acc_t{};
+    };
+    const auto masked = [&](int j) { return j * kBlock + kBlock - 1 > lim_lo; };
+    // (the table is asked before the length is known, and the first block is on its way before Q is waited for)
+    const bool there0 = block_here(blk);
+    // each wavefront on its own
+    const auto alone = [&]() {
+        asm volatile("" ::: "memory");  // (Q's loads stay on this side of the choice: in front of it they would be kept over the other loop)
+        uint4 qx[QS];
+        load_q(qx);
+        jb += kg;
+        if (jb < je) {
+            load_k(blk);
+            if constexpr (M == 16) load_v(blk);
+            scales_of(there0);
+        }
+        convert_q(qx);
+        clear();
+        if constexpr (M == 32) {  // (Q's two forms leave no registers for V)
+            if (jb < je) load_v(blk);
+        }
+        for (int j = jb; j < je; j += KW) {
+            if (j + KW < je) advance();  // (the last one fetches its own block again: no branch around the loads)
+            size_t nblk;
+            const bool there = block_here(nblk);
+            acc_t s[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < QS / 2; ++i) {
+                    const uint4 x = kx[t * (QS / 2) + i];
+                    s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), qh[2 * i], i == 0 ? acc_t{} : s[t]);
+                    s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), qh[2 * i + 1], s[t]);
+                    if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
+                }
+            load_k(nblk);
+            rescale(masked(j) ? softmax(std::true_type{}, s, j * kBlock) : softmax(std::false_type{}, s, 0));
+            // O^T += V^T P^T
+#pragma unroll
+            for (int t = 0; t < OT; ++t) {
+                if constexpr (M == 16) {
+                    const uint4 x = vx[t];
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), pb[0], o[t]);
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), pb[1], o[t]);
+                } else {
+                    const uint4 x = vx[2 * t], y = vx[2 * t + 1];
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, y.x), pb[0], o[t]);
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.y, y.y), pb[1], o[t]);
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, y.z), pb[2], o[t]);
+                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.w, y.w), pb[3], o[t]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            load_v(nblk);
+            blk = nblk;
+            scales_of(there);
+        }
+    };
+    const auto together = [&]() {
+        // The four wavefronts go through the same blocks: each turns a quarter of a block's codes into binary16 operands in LDS and all
+        // read them there.  The scores of block j + 1 are computed under the exponentials of block j, one matrix instruction to nine vector
+        // instructions, with the wavefront's priority raised; P V follows, with its operands four ahead.  A barrier per block.
+        // Measured, 4 sequences x 1024 rows x 4096 tokens, 32 heads over 8, not causal (a library's 16-bit product would take 225 us at its
+        // rate), INT8 / E4M3: each wavefront on its own 348 / 318 us, conversions shared 328 / 318, scores under the exponentials and operands
+        // ahead 315 / 304, priority raised 302 / 294; matrix pipe 37 % and vector issue 48 % of the time, and little of the two overlaps.  At
+        // d = 64, half the conversions, none of this is faster than a wavefront on its own (211 us; 208 to 215).
+        uint4 qx[QS];
+        load_q(qx);
+        uint8_t *stage = reinterpret_cast<uint8_t *>(acc_lds);
+        constexpr int KN = NL / kAttnWaves;
+        uint4 kq[KN], vq[2];
+        const auto fetch_k = [&](size_t at) {
+            const uint8_t *p = a.k + at * (kBlock * D) + k_lane;
+#pragma unroll
+            for (int i = 0; i < KN; ++i) kq[i] = *reinterpret_cast<const uint4 *>(p + k_at(KN * wave + i));
+        };
+        const auto fetch_v = [&](size_t at) {
+            const uint8_t *p = a.v + at * (kBlock * D) + v_lane;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) vq[i] = *reinterpret_cast<const uint4 *>(p + v_at(2 * wave + i));
+        };
+        const auto convert_k = [&](int buf) {
+            v8h *p = reinterpret_cast<v8h *>(stage + HALF * buf) + lane;
+#pragma unroll
+            for (int i = 0; i < KN; ++i) {
+                p[64 * (2 * (KN * wave + i))] = codes_to_half<E4M3>(kq[i].x, kq[i].y);
+                p[64 * (2 * (KN * wave + i) + 1)] = codes_to_half<E4M3>(kq[i].z, kq[i].w);
+            }
+        };
+        const auto convert_v = [&](int buf) {
+            v8h *p = reinterpret_cast<v8h *>(stage + HALF * (2 + buf)) + 256 * wave + lane;
+            p[0] = codes_to_half<E4M3>(vq[0].x, vq[1].x);
+            p[64] = codes_to_half<E4M3>(vq[0].y, vq[1].y);
+            p[128] = codes_to_half<E4M3>(vq[0].z, vq[1].z);
+            p[192] = codes_to_half<E4M3>(vq[0].w, vq[1].w);
+        };
+        const auto barrier = []() {  // for LDS alone: what was fetched ahead stays on its way
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        };
+        const int lim_all = last_key(tile * ROWS + rows - 1);
+        int je_all = lim_all < 0 ? 0 : lim_all / kBlock + 1;
+        if (split + 1 < a.splits) je_all = min(je_all, jb + a.split_blocks);
+        // Ahead of the block whose weights are computed: K by one (its scores are computed under the exponentials) and, in LDS, by two; V by one.
+        float ks1 = 0.0f, vs1 = 0.0f, ks2 = 0.0f, vs2 = 0.0f;
+        acc_t s0[KT], s1[KT];
+        size_t vblk = blk;  // the block behind the one that is fetched
+        const auto next_block = [&](int j) {  // (the last ones fetch a block again: no branch around the loads)
+            vblk = blk;
+            if (j < je_all) advance();
+            const bool there = block_here(blk);
+            ks2 = there ? scalar_load(a.k_scale + blk) : __builtin_nanf("");
+            vs2 = there ? scalar_load(a.v_scale + blk) : __builtin_nanf("");
+        };
+        const auto scores = [&](acc_t (&s)[KT], int buf) {
+            const v8h *p = reinterpret_cast<const v8h *>(stage + HALF * buf) + lane;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < QS; ++i) s[t] = Mfma<M>::run(p[64 * (t * QS + i)], qh[i], i == 0 ? acc_t{} : s[t]);
+        };
+        // block j: its scores are in `now`; the next one's go to `then`
+        const auto step = [&](int j, acc_t (&now)[KT], acc_t (&then)[KT], auto buf_c) {
+            constexpr int BUF = decltype(buf_c)::value;
+            if (j < je) {
+                float f;
+                const auto both = [&](auto masked_c) {
+                    __builtin_amdgcn_s_setprio(1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    scores(then, BUF ^ 1);
+                    f = softmax(masked_c, now, j * kBlock);
+                    // a matrix instruction, an operand four ahead, and what the vector unit does meanwhile
+                    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                    for (int i = 0; i < KT * QS; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, decltype(masked_c)::value ? 16 : 9, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(0);
+                };
+                if (masked(j)) both(std::true_type{});
+                else both(std::false_type{});
+                rescale(f);
+                __builtin_amdgcn_sched_barrier(0);
+                const v8h *p = reinterpret_cast<const v8h *>(stage + HALF * (2 + BUF)) + lane;
+#pragma unroll
+                for (int t = 0; t < OT; ++t)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) o[t] = Mfma<M>::run(p[64 * (4 * t + w)], pb[w], o[t]);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int i = 0; i < 4 * OT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            convert_k(BUF);
+            convert_v(BUF ^ 1);
+            ks = ks1, vs = vs1, ks1 = ks2, vs1 = vs2;
+            next_block(j + 3);
+            fetch_k(blk);
+            fetch_v(vblk);
+            barrier();
+        };
+        if (jb < je_all) {
+            fetch_k(blk);
+            fetch_v(blk);
+            scales_of(there0);
         }
-        load_v(nblk);
-        blk = nblk;
-        scales_of(there);
+        convert_q(qx);
+        clear();
+        if (jb < je_all) {
+            convert_k(0);
+            convert_v(0);
+            next_block(jb + 1);
+            fetch_k(blk);
+            fetch_v(blk);
+            ks1 = ks2, vs1 = vs2;
+            convert_k(1);
+            next_block(jb + 2);
+            fetch_k(blk);
+            barrier();
+            if (jb < je) scores(s0, 0);
+            barrier();
+            for (int j = jb; j < je_all; j += 2) {
+                step(j, s0, s1, std::integral_constant<int, 0>{});
+                if (j + 1 < je_all) step(j + 1, s1, s0, std::integral_constant<int, 1>{});
+            }
+        }
+    };
+    if constexpr (SHARED) {
+        if (RW == kAttnWaves) together();
+        else alone();
+    } else {
+        alone();
     }
     // a length beyond the table's row: what the row cannot hold is missing
     const float sum = Mfma<M>::row_sum(l) + (true_len > cap ? __builtin_nanf("") : 0.0f);
 
     // ---- the key groups' sums ----
-    const bool to_workspace = a.splits > 1;
+    const PagedArgs z = arguments_again();
     if (KW == 1) {
         if (lq >= mine) return;
-        const int ri = first + lq, tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
-        if (to_workspace && g == 0)
-            *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(m, sum);
-        if (to_workspace && m == -INFINITY && sum == 0.0f) return;  // (the combination does not read it)
+        const int ri = first + lq, tok = q0 + ri / z.group, hq = kvh * z.group + ri % z.group;
 #pragma unroll
         for (int t = 0; t < OT; ++t)
 #pragma unroll
             for (int i = 0; i < R; i += 4)
-                store_row_quad<D, BF16>(a, tok, hq, M * t + 2 * i + 4 * g,
-                                        make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref), sum,
-                                        to_workspace, split);
+                store_sums<D, BF16>(z, tok, hq, M * t + 2 * i + 4 * g,
+                                    make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref), m, sum, split);
         return;
     }
     {
@@ -345,7 +520,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     __syncthreads();
     for (int e = tid; e < rows * (D / 4); e += 64 * kAttnWaves) {
         const int r = e / (D / 4), ch = 4 * (e % (D / 4)), w0 = r / M, rr = r % M;
-        const int ri = tile * ROWS + r, tok = q0 + ri / a.group, hq = kvh * a.group + ri % a.group;
+        const int ri = tile * ROWS + r, tok = q0 + ri / z.group, hq = kvh * z.group + ri % z.group;
         float mx = -INFINITY;
         for (int w = w0; w < kAttnWaves; w += RW) mx = fmaxf(mx, ml_lds[w * M + rr].x);
         const float base = mx == -INFINITY ? 0.0f : mx;
@@ -358,10 +533,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
             all += f * ml.y;
             acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
         }
-        if (to_workspace && ch == 0)
-            *reinterpret_cast<float2 *>(a.part_ml + 2 * (((size_t)split * a.bt.T + tok) * a.Hq + hq)) = make_float2(mx, all);
-        if (to_workspace && mx == -INFINITY && all == 0.0f) continue;
-        store_row_quad<D, BF16>(a, tok, hq, ch, acc, all, to_workspace, split);
+        store_sums<D, BF16>(z, tok, hq, ch, acc, mx, all, split);
     }
 #endif  // __HIP_DEVICE_COMPILE__
 }
@@ -442,7 +614,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const PagedArgs a) {
         }
         sum = lanes(sum, [](float x, float y) { return x + y; });
     }
-    if (r < rows) store_row_quad<D, BF16>(a, tok, hq, 4 * e, acc, sum, false, 0);
+    if (r < rows) store_out<D, BF16>(a, tok, hq, 4 * e, acc, sum);
 }
 
 template <int D, bool BF16>
@@ -474,9 +646,13 @@ int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
     const int64_t workgroups = tiles * B * Hkv;
     const int64_t blocks = cdiv(max_len, kBlock);
     // Few workgroups: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than their
-    // wavefronts hide.  Many: up to four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least.
-    const int64_t ranges = workgroups < kCUs ? std::min((kCUs + workgroups / 2) / workgroups, std::max<int64_t>(1, blocks / 4))
-                                             : std::min(std::max<int64_t>(1, 4 * kCUs / workgroups), std::max<int64_t>(1, blocks / 32));
+    // wavefronts hide.  Many: with 16 rows up to four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least;
+    // with 32 rows two, which is what a CU holds.
+    int64_t ranges = std::min((kCUs + workgroups / 2) / workgroups, std::max<int64_t>(1, blocks / 4));
+    if (workgroups >= kCUs) {
+        ranges = rows == 16 * kAttnWaves ? 4 * kCUs / workgroups : (2 * kCUs + workgroups / 2) / workgroups;
+        ranges = std::max<int64_t>(1, std::min(ranges, blocks / 32));
+    }
     return (int)((blocks + ranges - 1) / ranges) * kBlock;
 }
 
