@@ -621,6 +621,7 @@ template <int D, bool BF16>
 void launch_merge(dim3 grid, hipStream_t stream, const PagedArgs &a) {
     if (a.splits <= 4) paged_merge_kernel<D, BF16, 4><<<grid, dim3(256), 0, stream>>>(a);
     else if (a.splits <= 16) paged_merge_kernel<D, BF16, 16><<<grid, dim3(256), 0, stream>>>(a);
+    else if (a.splits <= 32) paged_merge_kernel<D, BF16, 32><<<grid, dim3(256), 0, stream>>>(a);
     else paged_merge_kernel<D, BF16, 0><<<grid, dim3(256), 0, stream>>>(a);
 }
 

@@ -66,15 +66,38 @@ __device__ __forceinline__ int entry_of(const int *first, int n, int k) {
     return lo;
 }
 
+// Entry w of the row that a fork gives to dst, and the count of the page that it shares.
+__device__ __forceinline__ void fork_entry(const sage_page_table &pt, int src, int dst, int own, int len, int w) {
+    const int full = len / pt.page_tokens;
+    int page = -1;
+    if (w < full) {
+        page = pt.table[(size_t)src * pt.width + w];
+        if (page >= 0 && page < pt.n_pages) atomicAdd(pt.refs + page, 1);
+    } else if (w == full && len % pt.page_tokens) {
+        page = own;
+    }
+    pt.table[(size_t)dst * pt.width + w] = page;
+    if (w == 0) pt.lens[dst] = len;
+}
+
+// The second half of a fork where that is more than one workgroup's work: a workgroup per entry.
+__global__ __launch_bounds__(256) void fork_rows_kernel(const sage_page_table pt, const int32_t *__restrict__ page_moves,
+                                                        const int32_t *__restrict__ slot_moves) {
+    const int i = blockIdx.x, src = slot_moves[2 * i], dst = slot_moves[2 * i + 1];
+    if (dst < 0) return;
+    const int len = pt.lens[src];
+    for (int w = threadIdx.x; w < pt.width; w += 256) fork_entry(pt, src, dst, page_moves[2 * i + 1], len, w);
+}
+
 // Reserve (slots, n_new) and the first half of a fork (src, dst): one workgroup.  FORK: entry i needs one page if src's last page is not
-// full; its page and the moves are written here, tables and shared counts by fork_rows_kernel.
+// full; its page and the moves are written here, tables and shared counts too where rows_here, or by fork_rows_kernel.
 // Dynamic LDS: claim[slots] (the first entry that names a slot, of dst for forks), first[n + 1] (the pages needed before an entry), have[n]
 // (the pages that its row has, -1: refused).
 template <bool FORK, int EACH>
 __global__ __launch_bounds__(kThreads) void assign_kernel(const sage_page_table pt, const int32_t *__restrict__ slots,
                                                          const int32_t *__restrict__ n_new, const int32_t *__restrict__ src, int n,
                                                          int32_t *__restrict__ status, int32_t *__restrict__ page_moves,
-                                                         int32_t *__restrict__ slot_moves) {
+                                                         int32_t *__restrict__ slot_moves, bool rows_here) {
     constexpr int ROUND = kThreads * EACH;
     extern __shared__ int lds[];
     __shared__ int shared[kWaves];
@@ -169,27 +192,14 @@ __global__ __launch_bounds__(kThreads) void assign_kernel(const sage_page_table 
             pt.lens[slots[i]] += n_new ? n_new[i] : 1;  // (a slot is served once: nobody else looks at this length any more)
         }
     }
-}
-
-// The second half of a fork, a workgroup per entry: the row of dst, the counts of the pages that it shares.
-__global__ __launch_bounds__(256) void fork_rows_kernel(const sage_page_table pt, const int32_t *__restrict__ page_moves,
-                                                        const int32_t *__restrict__ slot_moves) {
-    const int i = blockIdx.x, src = slot_moves[2 * i], dst = slot_moves[2 * i + 1];
-    if (dst < 0) return;
-    const int len = pt.lens[src], full = len / pt.page_tokens;
-    const int32_t *from = pt.table + (size_t)src * pt.width;
-    int32_t *to = pt.table + (size_t)dst * pt.width;
-    for (int w = threadIdx.x; w < pt.width; w += 256) {
-        int page = -1;
-        if (w < full) {
-            page = from[w];
-            if (page >= 0 && page < pt.n_pages) atomicAdd(pt.refs + page, 1);
-        } else if (w == full && len % pt.page_tokens) {
-            page = page_moves[2 * i + 1];
+    if constexpr (FORK) {
+        if (!rows_here) return;
+        __syncthreads();
+        for (int e = tid; e < n * pt.width; e += kThreads) {
+            const int i = e / pt.width, s = slot_moves[2 * i], d = slot_moves[2 * i + 1];
+            if (d >= 0) fork_entry(pt, s, d, page_moves[2 * i + 1], pt.lens[s], e - i * pt.width);
         }
-        to[w] = page;
     }
-    if (threadIdx.x == 0) pt.lens[dst] = len;
 }
 
 // A workgroup per listed slot.  Entries are taken out by exchange, so a slot that is listed twice gives its pages back once.
@@ -279,14 +289,15 @@ size_t lds_bytes(const sage_page_table &pt, int n) { return ((size_t)pt.slots + 
 
 hipError_t launch_pages_reserve(const sage_page_table &pt, const int32_t *slots, const int32_t *n_new, int n, int32_t *status,
                                 hipStream_t stream) {
-    (pt.n_pages <= kSmallPool ? assign_kernel<false, kFew> : assign_kernel<false, kMany>)<<<dim3(1), dim3(kThreads), lds_bytes(pt, n), stream>>>(pt, slots, n_new, nullptr, n, status, nullptr, nullptr);
+    (pt.n_pages <= kSmallPool ? assign_kernel<false, kFew> : assign_kernel<false, kMany>)<<<dim3(1), dim3(kThreads), lds_bytes(pt, n), stream>>>(pt, slots, n_new, nullptr, n, status, nullptr, nullptr, false);
     return hipGetLastError();
 }
 
 hipError_t launch_pages_fork(const sage_page_table &pt, const int32_t *src, const int32_t *dst, int n, int32_t *status, int32_t *page_moves,
                              int32_t *slot_moves, hipStream_t stream) {
-    (pt.n_pages <= kSmallPool ? assign_kernel<true, kFew> : assign_kernel<true, kMany>)<<<dim3(1), dim3(kThreads), lds_bytes(pt, n), stream>>>(pt, dst, nullptr, src, n, status, page_moves, slot_moves);
-    fork_rows_kernel<<<dim3(n), dim3(256), 0, stream>>>(pt, page_moves, slot_moves);
+    const bool rows_here = (int64_t)n * pt.width <= 8 * kThreads;  // a few rounds of one workgroup against a launch
+    (pt.n_pages <= kSmallPool ? assign_kernel<true, kFew> : assign_kernel<true, kMany>)<<<dim3(1), dim3(kThreads), lds_bytes(pt, n), stream>>>(pt, dst, nullptr, src, n, status, page_moves, slot_moves, rows_here);
+    if (!rows_here) fork_rows_kernel<<<dim3(n), dim3(256), 0, stream>>>(pt, page_moves, slot_moves);
     return hipGetLastError();
 }
 
