@@ -392,7 +392,7 @@ typedef enum { SAGE_CACHE_I8 = 0, SAGE_CACHE_E4M3 = 1 } sage_cache_format;
 typedef struct {
     int32_t *table;  /* device, [slots][width]: page ids, -1 where there is none */
     int32_t *lens;   /* device, [slots]: tokens of each slot, 0 if it is free    */
-    int32_t *refs;   /* device, [n_pages]: slots that name a page, 0 if it is free */
+    int32_t *refs;   /* device, [n_pages], 16-byte aligned: slots that name a page, 0 if it is free */
     int slots;       /* 1 .. SAGE_MAX_SLOTS */
     int width;       /* pages a slot can have, >= 1; width * page_tokens <= 2^22 */
     int n_pages;     /* 1 .. 2^22 */
@@ -413,8 +413,9 @@ typedef struct {
 
 /* The T rows of a call belong to B sequences: rows q_start[b] .. q_start[b+1]-1 (device int32 [B+1], ascending, within 0 .. T) to the
  * b-th, or T/B rows each where q_start is NULL (T a multiple of B).  Rows that belong to none are neither read nor written.
- * slots[b] (device int32 [B], or NULL for b itself) is the sequence's slot; a sequence whose slot is outside the table
- * is padding: its rows are skipped too. */
+ * slots[b] (device int32 [B], or NULL for b itself, then B <= slots) is the sequence's slot; a sequence whose slot is outside the table
+ * is padding: its rows are skipped too.  1 <= T, B <= 2^22, and T * Hq <= 2^30.  Sizes that would take a launch of more than 2^23
+ * workgroups in one dimension are refused (SAGE_EINVAL). */
 
 /* ---- rotary positions --------------------------------------------------- */
 

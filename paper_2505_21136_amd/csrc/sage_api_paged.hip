@@ -12,7 +12,7 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 bool ok4(const void *p) { return p && aligned4(p); }
 
 constexpr int kMaxTokens = 1 << 22;
-constexpr int64_t kMaxWorkgroups = 1 << 23;  // of a launch (a grid's threads are counted in 32 bits)
+constexpr int64_t kMaxWorkgroups = 1 << 23;  // of a launch's first dimension (its threads are counted in 32 bits)
 
 bool table_ok(const sage_page_table *pt) {
     return pt && ok4(pt->table) && ok4(pt->lens) && ok16(pt->refs) && pt->slots >= 1 && pt->slots <= SAGE_MAX_SLOTS && pt->width >= 1 &&
@@ -129,7 +129,7 @@ int sage_paged_append(const sage_page_table *pages, const sage_cache *cache, con
     if (!table_ok(pages) || !cache_ok(cache) || !ok16(k) || !ok16(v) || !batch_ok(q_start, slots, B, T, pages, &bt)) return SAGE_EINVAL;
     if (!read_strides(k_strides, cache->Hkv, cache->d, &ks) || !read_strides(v_strides, cache->Hkv, cache->d, &vs)) return SAGE_EINVAL;
     if (rope && !plan_ok(rope, cache->d)) return SAGE_EINVAL;
-    if (((int64_t)T / 64 + 2 * (int64_t)B) * 2 * cache->Hkv > kMaxWorkgroups) return SAGE_EINVAL;
+    if ((int64_t)T / 64 + 2 * (int64_t)B > kMaxWorkgroups) return SAGE_EINVAL;
     discard_pending_hip_error();
     return sage::status_of(sage::launch_paged_append(*pages, *cache, k, ks, v, vs, bt, rope, static_cast<hipStream_t>(stream)));
 }
@@ -139,14 +139,14 @@ int sage_paged_gather(const sage_page_table *pages, const sage_cache *cache, voi
     sage::Batch bt;
     if (!table_ok(pages) || !cache_ok(cache) || !ok16(k_out) || !ok16(v_out) || !k_start) return SAGE_EINVAL;
     if (!batch_ok(k_start, slots, B, total, pages, &bt)) return SAGE_EINVAL;
-    if (((int64_t)total / 64 + B) * 2 * cache->Hkv > kMaxWorkgroups) return SAGE_EINVAL;
+    if ((int64_t)total / 64 + B > kMaxWorkgroups) return SAGE_EINVAL;
     discard_pending_hip_error();
     return sage::status_of(sage::launch_paged_gather(*pages, *cache, k_out, v_out, bt, static_cast<hipStream_t>(stream)));
 }
 
 static bool paged_sizes_ok(int T, int B, int Hq, int Hkv, int max_len, int split_keys) {
     return T >= 1 && T <= kMaxTokens && B >= 1 && B <= kMaxTokens && Hkv >= 1 && Hkv <= 1024 && Hq >= 1 && Hq <= 65536 && Hq % Hkv == 0 &&
-           max_len >= 1 && max_len <= kMaxTokens && split_keys >= 0 && split_keys <= kMaxTokens && split_keys % SAGE_CACHE_BLOCK == 0;
+           (int64_t)T * Hq <= (1 << 30) && max_len >= 1 && max_len <= kMaxTokens && split_keys >= 0 && split_keys <= kMaxTokens && split_keys % SAGE_CACHE_BLOCK == 0;
 }
 
 int sage_paged_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
@@ -171,7 +171,7 @@ int sage_attn_fwd_paged(const void *q, void *out, const int64_t *q_strides, cons
         return SAGE_EINVAL;
     if (split_keys == 0) split_keys = sage::paged_auto_split_keys(T, B, Hq, cache->Hkv, max_len);
     const sage::PagedScratch ws = sage::paged_scratch_layout(workspace, T, Hq, cache->d, max_len, split_keys);
-    if (ws.splits > 65535 || sage::paged_attn_workgroups(T, B, Hq, cache->Hkv, q_start != nullptr, ws.splits) > kMaxWorkgroups)
+    if (ws.splits > 65535 || sage::paged_attn_workgroups(T, B, Hq, cache->Hkv, cache->d, q_start != nullptr, ws.splits) > kMaxWorkgroups)
         return SAGE_EINVAL;
     if (ws.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < ws.bytes)) return SAGE_EWORKSPACE;
     if (!(isfinite(sm_scale) && sm_scale > 0.0f)) sm_scale = 1.0f / sqrtf((float)cache->d);

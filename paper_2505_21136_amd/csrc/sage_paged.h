@@ -145,7 +145,7 @@ struct PagedScratch {
 };
 int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len);
 PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len, int split_keys);
-int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, bool ragged, int splits);
+int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, int d, bool ragged, int splits);  // the most of a launch's first dimension
 hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenStrides o_st, const sage_page_table &pt, const sage_cache &c,
                              const Batch &bt, int Hq, bool causal, float sm_scale, int split_keys, const PagedScratch &ws, hipStream_t stream);
 

@@ -284,11 +284,17 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(const GatherArgs a) {
                 sh[4 * i] = s.x, sh[4 * i + 1] = s.y, sh[4 * i + 2] = s.z, sh[4 * i + 3] = s.w;
             }
         }
+        uint4 w2[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {  // (all 64 tokens are there: no branch around the loads)
+            const int r = tid / (D / 16) + 32 * e;
+            w2[e] = *reinterpret_cast<const uint4 *>(codes + (((r >> 4) * (D / 64) + (item >> 2)) * 64 + (item & 3) * 16 + (r & 15)) * 16);
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = tid / (D / 16) + 32 * e;
             if (r >= rows) continue;
-            const uint4 w = *reinterpret_cast<const uint4 *>(codes + (((r >> 4) * (D / 64) + (item >> 2)) * 64 + (item & 3) * 16 + (r & 15)) * 16);
+            const uint4 w = w2[e];
             const uint32_t c[4] = {w.x, w.y, w.z, w.w};
             uint32_t y[8];
 #pragma unroll

@@ -668,8 +668,9 @@ PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len,
     return w;
 }
 
-int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, bool ragged, int splits) {
-    return row_slots(T, B, Hq / Hkv, 8, ragged) * Hkv * splits;  // (an upper bound for both kernels)
+int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, int d, bool ragged, int splits) {
+    const int group = Hq / Hkv;
+    return Hkv * std::max(row_slots(T, B, group, kAttnWaves * wave_rows(T, B, group), ragged), splits > 1 ? row_slots(T, B, group, 1024 / d, ragged) : 0);
 }
 
 hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenStrides o_st, const sage_page_table &pt, const sage_cache &c,

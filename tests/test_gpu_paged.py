@@ -336,6 +336,15 @@ def test_chunks_and_single_tokens_together(fmt, dtype, d, causal):
     run_case([400, 129, 77, 1, 260, 64], [130, 1, 77, 1, 33, 0], Hq=4, Hkv=2, d=d, dtype=dtype, fmt=fmt, page=192, causal=causal, seed=9, split=128)
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_chunks(fmt, dtype, causal):
+    # tiles of 128 rows over an odd and an even number of blocks, in one range and in three; the last tile is short
+    for lens, split in (([705, 1024], 0), ([705, 1024], 384)):
+        run_case(lens, [150, 200], Hq=6, Hkv=2, d=128, dtype=dtype, fmt=fmt, page=64, causal=causal, seed=21, split=split)
+
+
 def test_rows_that_see_nothing_are_zeros():
     # more rows than tokens: the first ones lie in front of the sequence
     for split in (0, 64):
@@ -540,6 +549,73 @@ def test_a_captured_step_replays_as_sequences_grow():
     for a, b in zip(sage.sage_paged_gather(cache, ints(0, *torch.tensor(n).cumsum(0).tolist()), sum(n)),
                     sage.sage_paged_gather(cache2, ints(0, *torch.tensor(n).cumsum(0).tolist()), sum(n))):
         assert torch.equal(a, b)
+
+
+def test_captured_upkeep():
+    """Fork, copy, free, compaction and reading back in one graph: every replay, from a table that changed in between, against the eager calls."""
+    B, Hkv, d, dt = 3, 2, 64, torch.float16
+    slots, n_pages = 8, 24
+    sets = [empty(slots, Hkv, d, dt, "e4m3", 64, 6, n_pages=n_pages) for _ in range(2)]
+    src, dst, gone, starts = ints(1, 2, 1), ints(4, 5, 6), ints(1, 0), ints(0, 200, 300, 400)
+
+    def work(pages, cache):
+        status, moves, slot_moves = sage.sage_pages_fork(pages, src, dst)
+        sage.sage_pages_copy(cache, moves, slot_moves)
+        sage.sage_pages_free(pages, gone)
+        moves, counts = sage.sage_pages_compact(pages)
+        sage.sage_pages_copy(cache, moves)
+        return status, counts, *sage.sage_paged_gather(cache, starts, 400, slots=dst)
+
+    def fill(pages, cache, lens, k):
+        sage.sage_pages_free(pages, torch.arange(slots, dtype=torch.int32, device=DEV))
+        sage.sage_pages_reserve(pages, ints(*lens), ints(0, 1, 2))
+        sage.sage_paged_append(cache, k, -k, q_start=ints(0, *torch.tensor(lens).cumsum(0).tolist()), slots=ints(0, 1, 2))
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    first = torch.randn(150, Hkv, d, device=DEV).to(dt)
+    fill(*sets[0], [10, 70, 70], first)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        got = work(*sets[0])
+    for lens in ([10, 70, 70], [300, 128, 1], [64, 200, 90], [10, 70, 70]):
+        k = torch.randn(sum(lens), Hkv, d, device=DEV).to(dt)
+        for s in sets:
+            fill(*s, lens, k)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = work(*sets[1])
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), lens
+        assert torch.equal(sets[0][0].table, sets[1][0].table) and torch.equal(sets[0][0].refs, sets[1][0].refs)
+
+
+def test_two_graphs_share_a_workspace_and_two_streams_do_not():
+    cache = make_cache([700, 300], Hkv=2, d=64, dtype=torch.bfloat16, fmt="int8", page_tokens=64, seed=5)
+    q = [torch.randn(2, 8, 64, device=DEV).bfloat16() for _ in range(2)]
+    kw = dict(causal=True, max_len=700, split_keys=64)
+    want = [sage.sage_attn_fwd_paged(x, cache, **kw) for x in q]
+    ws = torch.empty(sage.paged_workspace_bytes(2, 2, 8, 2, 64, 700, 64), dtype=torch.uint8, device=DEV)
+    outs, graphs, side = [torch.zeros_like(x) for x in q], [torch.cuda.CUDAGraph() for _ in q], torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for x, o, g in zip(q, outs, graphs):
+        with torch.cuda.graph(g, stream=side):
+            sage.sage_attn_fwd_paged(x, cache, out=o, workspace=ws, **kw)
+    for i in (0, 1, 1, 0, 1):
+        outs[i].zero_()
+        ws.fill_(255)                                     # nothing in it has to be initialised
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want[i])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(5):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i] = sage.sage_attn_fwd_paged(q[i], cache, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_refusals_on_the_device():

@@ -116,8 +116,9 @@ def test_refusals_of_the_calls():
     for bad in (dict(q=None), dict(q=p + 8), dict(out=None), dict(B=0), dict(T=0), dict(B=3), dict(B=9, T=9), dict(Hq=7), dict(Hq=0), dict(max_len=0),
                 dict(max_len=(1 << 22) + 1), dict(split=-64), dict(split=32), dict(q_start=p + 2), dict(slots=p + 1), dict(qs=st(-8, 128)),
                 dict(qs=st(1024, 4)), dict(qs=st(1 << 41, 128)), dict(os_=st(1024, 64)), dict(os_=st(512, 128)), dict(os_=st(0, 128)),
-                dict(T=(1 << 22) + 4), dict(T=1 << 22, max_len=1 << 22)):
+                dict(T=(1 << 22) + 4), dict(T=1 << 22, Hq=512), dict(T=1 << 22, max_len=1 << 22, split=64), dict(T=1 << 22, Hq=64, max_len=640)):
         assert attn(**bad) == EINVAL, bad
+    assert attn(T=1 << 22, max_len=640) == EWS                                  # the limit itself passes
     assert attn(q_start=p, B=3) == EWS and attn(slots=p, B=64, T=64) == EWS and attn(qs=st(0, 0)) == EWS and attn(os_=st(128, 512)) == EWS
     assert sage.paged_workspace_bytes(4, 4, 8, 2, 128, 512, 512) == 0           # one range: none needed
     assert sage.paged_workspace_bytes(4, 4, 8, 2, 128, 512, 64) == 8 * 4 * 8 * (128 + 2) * 4
