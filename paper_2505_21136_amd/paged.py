@@ -289,28 +289,24 @@ def sage_pages_reserve(pages: PageTable, n_new: torch.Tensor | None = None, slot
     """n_new[i] more tokens (int32, or None: 1 each) for slots[i] (None: all slots): -> status int32, 0 or -1 (refused)."""
     if slots is None:
         slots = torch.arange(pages.slots, dtype=torch.int32, device=pages.table.device)
-    _here(pages.table, "the page table")
-    status = torch.empty_like(slots)
-    _sage._check(_sage.lib().sage_pages_reserve(pages.ref, _ints(slots, "slots"), _ints(n_new, "n_new", slots.numel()), slots.numel(),
-                                                status.data_ptr(), _sage._stream()))
+    at, n = _ints(slots, "slots"), slots.numel()
+    status = slots.new_empty(n)
+    _sage._check(_sage.lib().sage_pages_reserve(pages.ref, at, _ints(n_new, "n_new", n), n, status.data_ptr(), _sage._stream()))
     return status
 
 
 def sage_pages_fork(pages: PageTable, src: torch.Tensor, dst: torch.Tensor):
     """Slot dst[i] becomes a copy of slot src[i]: -> (status [n], page_moves [n, 2], slot_moves [n, 2]); sage_pages_copy then copies in
     each layer's cache."""
-    n = src.numel()
-    status = torch.empty_like(src)
-    moves = torch.empty((2, n, 2), dtype=torch.int32, device=src.device)
-    _here(pages.table, "the page table")
-    _sage._check(_sage.lib().sage_pages_fork(pages.ref, _ints(src, "src"), _ints(dst, "dst", n), n, status.data_ptr(), moves[0].data_ptr(),
-                                             moves[1].data_ptr(), _sage._stream()))
-    return status, moves[0], moves[1]
+    at, n = _ints(src, "src"), src.numel()
+    status, moves = src.new_empty(n), src.new_empty((2, n, 2))
+    p = moves.data_ptr()
+    _sage._check(_sage.lib().sage_pages_fork(pages.ref, at, _ints(dst, "dst", n), n, status.data_ptr(), p, p + 8 * n, _sage._stream()))
+    return (status, *moves.unbind())
 
 
 def sage_pages_free(pages: PageTable, slots: torch.Tensor) -> None:
     """The listed slots' pages are given back; the slots are empty afterwards."""
-    _here(pages.table, "the page table")
     _sage._check(_sage.lib().sage_pages_free(pages.ref, _ints(slots, "slots"), slots.numel(), _sage._stream()))
 
 
@@ -318,11 +314,9 @@ def sage_pages_compact(pages: PageTable, max_moves: int | None = None, *, worksp
     """Live pages move to the front of the pool: -> (page_moves [max_moves, 2], counts [2] = {live pages, moves}); sage_pages_copy then
     copies in each layer's cache."""
     most = max(1, pages.n_pages // 2) if max_moves is None else int(max_moves)
-    dev = pages.table.device
     _here(pages.table, "the page table")
-    moves = torch.empty((max(most, 0), 2), dtype=torch.int32, device=dev)
-    counts = torch.empty(2, dtype=torch.int32, device=dev)
-    ws = workspace if workspace is not None else _sage._workspace(int(_sage.lib().sage_pages_compact_workspace_bytes(pages.n_pages)), dev)
+    moves, counts = pages.refs.new_empty((max(most, 0), 2)), pages.refs.new_empty(2)
+    ws = workspace if workspace is not None else pages.refs.new_empty((pages.n_pages + 63) // 64 * 64)
     _sage._check(_sage.lib().sage_pages_compact(pages.ref, moves.data_ptr(), most, counts.data_ptr(), _sage._stream(), ws.data_ptr(),
                                                 ws.numel() * ws.element_size()))
     return moves, counts
