@@ -57,9 +57,9 @@ struct AppendArgs {
 //      or two runs of 8.
 //   V: a thread takes 2 channels of the 16 tokens whose codes are neighbours in the cache, 16 bytes per channel; a wavefront's loads are
 //      whole rows of 256 bytes.
-// Bound by memory where there is much of it (one prompt of 32768 tokens x 8 heads x 128: 42 us = 4.8 TB/s; 64 sequences' one token each, 8 KB of tail
-// read and 8 KB of codes written per head: 9.8 us, 512 35 us), by the chain length -- tokens -- maximum -- codes where there is little (one
-// sequence 5.4 us; ten ragged prompts of 12600 tokens, rotated, 28 us).
+// Bound by memory where there is much of it (one prompt of 32768 tokens x 8 heads x 128: 39 us = 5.2 TB/s; 64 sequences' one token each, 8 KB of tail
+// read and 8 KB of codes written per head: 10 us, 512 36 us), by the chain length -- tokens -- maximum -- codes where there is little (one
+// sequence 5.4 us; ten ragged prompts of 12600 tokens, rotated, 27 us).
 // Values stay in registers in 16 bits and are widened twice, for the maximum and for the codes: 80 registers, six wavefronts per SIMD, which
 // the chain table -- tokens -- maximum -- codes needs to keep memory busy.
 // The tail's two halves hold the tokens of the sequence's last two blocks.  The half that the first touched block stands in is
@@ -119,10 +119,16 @@ __device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_ro
             for (int e = 0; e < 2; ++e)
                 if (p0 + r0 + 32 * e >= len) kw[e][0] = kw[e][1] = make_uint4(0, 0, 0, 0);
         } else {
+            if (p0 >= start && p0 + kBlock <= len) {  // all new, all there: one row's address, the others at uniform distances
+                const uint16_t *r = row_of(p0 + 4 * g) + 2 * cp;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) vw[i] = *reinterpret_cast<const uint32_t *>(row_of(min(p0 + v_token(i), len - 1)) + 2 * cp);
+                for (int i = 0; i < 16; ++i) vw[i] = *reinterpret_cast<const uint32_t *>(r + (int64_t)(v_token(i) - 4 * g) * st.t);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) vw[i] = p0 + v_token(i) < len ? vw[i] : 0;
+                for (int i = 0; i < 16; ++i) vw[i] = *reinterpret_cast<const uint32_t *>(row_of(min(p0 + v_token(i), len - 1)) + 2 * cp);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) vw[i] = p0 + v_token(i) < len ? vw[i] : 0;
+            }
         }
     };
     // eight values in binary32: K: run o of token e (2 e + o); V: channel ch's tokens 8 u .. (2 ch + u)
