@@ -654,14 +654,17 @@ int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
     const int64_t workgroups = tiles * B * Hkv;
     const int64_t blocks = cdiv(max_len, kBlock);
     // Few workgroups: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than their
-    // wavefronts hide.  Many: with 16 rows up to four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least;
-    // with 32 rows two, which is what a CU holds.
-    int64_t ranges = std::min((kCUs + workgroups / 2) / workgroups, std::max<int64_t>(1, blocks / 4));
-    if (workgroups >= kCUs) {
-        ranges = rows == 16 * kAttnWaves ? 4 * kCUs / workgroups : (2 * kCUs + workgroups / 2) / workgroups;
-        ranges = std::max<int64_t>(1, std::min(ranges, blocks / 32));
-    }
-    return (int)((blocks + ranges - 1) / ranges) * kBlock;
+    // wavefronts hide -- and none up to twelve blocks, where the second launch costs more than it saves (32 heads over 8, one sequence, us: 768
+    // tokens 8.5 in one range and 8.9 in three at d 128, 7.0 and 8.0 at d 64; 1280 tokens 10.6 and 9.7, 8.7 and 8.7).  Many: with 16 rows up to
+    // four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least (48 sequences of 1000 to 8192 tokens, d 128: one
+    // range 102, two 96, four 96, eight 96, sixteen 103); with 32 rows two, which is what a CU holds (six sequences, up to 512 rows over up to
+    // 16384 tokens: one range 454, two 284, four 305, eight 342).
+    int64_t ranges;
+    if (workgroups < kCUs) ranges = blocks <= 12 ? 1 : std::min((kCUs + workgroups / 2) / workgroups, blocks / 4);
+    else ranges = std::min(rows == 16 * kAttnWaves ? 4 * kCUs / workgroups : (2 * kCUs + workgroups / 2) / workgroups, blocks / 32);
+    ranges = std::max<int64_t>(1, ranges);
+    // a multiple of four blocks: four wavefronts share a range's keys (1280 tokens, d 128: ranges of five blocks 9.8 us, of four 8.9)
+    return (int)(((blocks + ranges - 1) / ranges + 3) / 4 * 4) * kBlock;
 }
 
 PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len, int split_keys) {
