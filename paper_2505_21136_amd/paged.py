@@ -76,6 +76,12 @@ def _here(t: torch.Tensor, what: str) -> None:
         raise _sage.SageError(f"{what} is on device {device}, the current device is {_current()}")
 
 
+def _ours(pages: "PageTable") -> None:
+    """The table, and with it the caches over it, lives on the device that the launches go to."""
+    if pages.device_index != _current():
+        raise _sage.SageError(f"the page table is on device {pages.device_index}, the current device is {_current()}")
+
+
 def _ints(t: torch.Tensor | None, what: str, n: int | None = None) -> int | None:
     """The address of a contiguous int32 list (of n entries)."""
     if t is None:
@@ -157,6 +163,7 @@ class PageTable:
         self._c = _PageTable(table.data_ptr(), _ints(lens, "lens", self.slots), _ints(refs, "refs"), self.slots, self.width, self.n_pages,
                              self.page_tokens)
         self.ref = ctypes.byref(self._c)
+        self.device_index = table.get_device()
 
     @classmethod
     def empty(cls, n_pages: int, *, page_tokens: int, slots: int, width: int, device="cuda") -> "PageTable":
@@ -172,6 +179,7 @@ class PagedCache:
     def __init__(self, pages: PageTable, *, k, v, k_scale, v_scale, k_tail, v_tail, fmt: str = "int8", k_shift: torch.Tensor | None = None):
         if fmt not in FORMATS:
             raise _sage.SageError(f"fmt is one of {sorted(FORMATS)}")
+        _ours(pages)
         if k_tail.dim() != 4:
             raise _sage.SageError("k_tail must be [slots, Hkv, 128, d]")
         Hkv, d = k_tail.shape[1], k_tail.shape[3]
@@ -231,6 +239,7 @@ def sage_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, *, q_
     ks, vs = _of_cache(k, cache, "k", cache.Hkv), _of_cache(v, cache, "v", cache.Hkv)
     if k.shape != v.shape:
         raise _sage.SageError("k and v must have one shape")
+    _ours(cache.pages)
     B = _batch(cache, q_start, slots, "q_start")
     _sage._check(_sage.lib().sage_paged_append(
         cache.pages.ref, cache.ref, k.data_ptr(), v.data_ptr(), ks, vs, _ints(q_start, "q_start"), _ints(slots, "slots", B), B, k.shape[0],
@@ -240,10 +249,10 @@ def sage_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, *, q_
 def sage_paged_gather(cache: PagedCache, k_start: torch.Tensor, total: int, *, slots: torch.Tensor | None = None):
     """The tokens of sequence b as rows k_start[b] .. k_start[b + 1] - 1 of (k, v), [total, Hkv, d] in 16 bits; rows of no sequence are
     left unwritten."""
+    _ours(cache.pages)
     B = _batch(cache, k_start, slots, "k_start")
     k = cache.k_tail.new_empty((total, cache.Hkv, cache.d))
     v = cache.k_tail.new_empty((total, cache.Hkv, cache.d))
-    _here(k, "the cache")
     _sage._check(_sage.lib().sage_paged_gather(cache.pages.ref, cache.ref, k.data_ptr(), v.data_ptr(), _ints(k_start, "k_start"),
                                                _ints(slots, "slots", B), B, int(total), _sage._stream()))
     return k, v
@@ -273,6 +282,7 @@ def sage_attn_fwd_paged(q: torch.Tensor, cache: PagedCache, *, causal: bool, max
         os_ = _of_cache(out, cache, "out")
         if out.shape != q.shape:
             raise _sage.SageError("out must have q's shape")
+    _ours(cache.pages)
     B = _batch(cache, q_start, slots, "q_start")
     if workspace is None:
         workspace = _sage._workspace(paged_workspace_bytes(T, B, Hq, cache.Hkv, d, max_len, split_keys), q.device)
@@ -287,6 +297,7 @@ def sage_attn_fwd_paged(q: torch.Tensor, cache: PagedCache, *, causal: bool, max
 
 def sage_pages_reserve(pages: PageTable, n_new: torch.Tensor | None = None, slots: torch.Tensor | None = None) -> torch.Tensor:
     """n_new[i] more tokens (int32, or None: 1 each) for slots[i] (None: all slots): -> status int32, 0 or -1 (refused)."""
+    _ours(pages)
     if slots is None:
         slots = torch.arange(pages.slots, dtype=torch.int32, device=pages.table.device)
     at, n = _ints(slots, "slots"), slots.numel()
@@ -298,6 +309,7 @@ def sage_pages_reserve(pages: PageTable, n_new: torch.Tensor | None = None, slot
 def sage_pages_fork(pages: PageTable, src: torch.Tensor, dst: torch.Tensor):
     """Slot dst[i] becomes a copy of slot src[i]: -> (status [n], page_moves [n, 2], slot_moves [n, 2]); sage_pages_copy then copies in
     each layer's cache."""
+    _ours(pages)
     at, n = _ints(src, "src"), src.numel()
     status, moves = src.new_empty(n), src.new_empty((2, n, 2))
     p = moves.data_ptr()
@@ -307,6 +319,7 @@ def sage_pages_fork(pages: PageTable, src: torch.Tensor, dst: torch.Tensor):
 
 def sage_pages_free(pages: PageTable, slots: torch.Tensor) -> None:
     """The listed slots' pages are given back; the slots are empty afterwards."""
+    _ours(pages)
     _sage._check(_sage.lib().sage_pages_free(pages.ref, _ints(slots, "slots"), slots.numel(), _sage._stream()))
 
 
@@ -314,7 +327,9 @@ def sage_pages_compact(pages: PageTable, max_moves: int | None = None, *, worksp
     """Live pages move to the front of the pool: -> (page_moves [max_moves, 2], counts [2] = {live pages, moves}); sage_pages_copy then
     copies in each layer's cache."""
     most = max(1, pages.n_pages // 2) if max_moves is None else int(max_moves)
-    _here(pages.table, "the page table")
+    _ours(pages)
+    if workspace is not None:
+        _here(workspace, "workspace")
     moves, counts = pages.refs.new_empty((max(most, 0), 2)), pages.refs.new_empty(2)
     ws = workspace if workspace is not None else pages.refs.new_empty((pages.n_pages + 63) // 64 * 64)
     _sage._check(_sage.lib().sage_pages_compact(pages.ref, moves.data_ptr(), most, counts.data_ptr(), _sage._stream(), ws.data_ptr(),
@@ -335,5 +350,5 @@ def sage_pages_copy(cache: PagedCache, page_moves: torch.Tensor | None, slot_mov
     """Carry out the moves of sage_pages_fork or sage_pages_compact in one layer's cache."""
     pm, n = _moves(page_moves, "page_moves")
     sm, ns = _moves(slot_moves, "slot_moves")
-    _here(cache.k, "the cache")
+    _ours(cache.pages)
     _sage._check(_sage.lib().sage_pages_copy(cache.pages.ref, cache.ref, pm, n, sm, ns, _sage._stream()))

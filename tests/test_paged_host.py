@@ -178,6 +178,23 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         sage.PageTable.empty(4, page_tokens=64, slots=2, width=2, device="cpu")
 
 
+def test_binding_refuses_a_table_on_another_device(monkeypatch):
+    """Every call that launches on the current device looks at where its table is, whatever the other tensors say."""
+    pages, cache = object.__new__(sage.PageTable), object.__new__(sage.PagedCache)
+    pages.device_index, pages.slots, pages.n_pages, pages.page_tokens, pages.ref = 1, 4, 4, 64, None
+    cache.pages, cache.Hkv, cache.d, cache.dtype, cache.ref = pages, 2, 64, torch.float16, None
+    monkeypatch.setattr(paged, "_current", lambda: 0)
+    monkeypatch.setattr(paged, "_here", lambda t, what: None)
+    x, i = torch.zeros(4, 2, 64, dtype=torch.float16), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: sage.sage_paged_append(cache, x, x), lambda: sage.sage_paged_gather(cache, i, 4),
+                 lambda: sage.sage_attn_fwd_paged(x, cache, causal=True, max_len=64), lambda: sage.sage_pages_reserve(pages),
+                 lambda: sage.sage_pages_reserve(pages, i, i), lambda: sage.sage_pages_fork(pages, i, i), lambda: sage.sage_pages_free(pages, i),
+                 lambda: sage.sage_pages_compact(pages), lambda: sage.sage_pages_copy(cache, torch.zeros(1, 2, dtype=torch.int32)),
+                 lambda: sage.PagedCache(pages, k=x, v=x, k_scale=x, v_scale=x, k_tail=x, v_tail=x)):
+        with pytest.raises(sage.SageError, match="the page table is on device 1, the current device is 0"):
+            call()
+
+
 def test_table_simulation_is_consistent():
     class Pages:
         page_tokens, width = 64, 4
