@@ -1,14 +1,14 @@
 // Attention over the paged 8-bit cache (gfx950; not treated in the paper): rows of any number per sequence, one kernel.
 //
-// S^T = K Q^T and O^T = V^T P^T in 16-bit matrix instructions (16x16x32) with binary32 accumulators; the codes of K and V become binary16
+// S^T = K Q^T and O^T = V^T P^T in 16-bit matrix instructions (16x16x32, 32x32x16) with binary32 accumulators; the codes of K and V become binary16
 // in registers, exactly.  The scales of a block of 64 keys are one number each for K and V: K's goes into the softmax's constant, V's, relative to
 // the largest so far, into P~ before it is rounded.  One pass over the keys with running maximum and sum.
 //
 // The cache keeps the bytes of a block in the order of the operands, so a wavefront loads 1 KB of neighbouring bytes at a time
-// straight into registers; nothing of K, V or P passes through LDS and the loop has no barrier.  The rows of all query heads that share a
-// K/V head are packed, token by token, into tiles of 16 or 32: the cache of a head is read once for all of them.
+// straight into registers; nothing of K, V or P passes through LDS and the loop has no barrier (128 rows at d = 128 excepted, below).  The rows of all query heads that share a
+// K/V head are packed, token by token, into tiles of 16, 32 or 48: the cache of a head is read once for all of them.
 //
-// A workgroup is four wavefronts of 16 or 32 rows.  With no more rows than one wavefront takes, the four share the keys (wavefront w takes
+// A workgroup is four wavefronts of 16, 32 or 48 rows.  With no more rows than one wavefront takes, the four share the keys (wavefront w takes
 // every fourth block; the partial sums meet in LDS at the end); with more, each wavefront, or each two, have rows of their own.
 //
 // What bounds it.  Up to 16 rows per K/V head: memory; 64 sequences x 16384 tokens, 32 heads over 8, d 128: 360 us = 6.0 TB/s, 95 % of what a read
@@ -124,21 +124,21 @@ struct Mfma<32> {
     static __device__ __forceinline__ float row_sum(float x) { return halves_sum(x); }
 };
 
-// D: head dimension; M: rows per wavefront, 16 or 32.
-template <int D, bool BF16, bool E4M3, int M>
-__global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_kernel(const PagedArgs a) {
+// D: head dimension; M: rows of a matrix instruction, 16 or 32; NT: how many times that a wavefront takes.
+template <int D, bool BF16, bool E4M3, int M, int NT>
+__global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_rows_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int NL = D / 16;       // loads of 16 bytes a lane for a block of K, and of V
     constexpr int R = M * M / 64;    // registers of an accumulator tile
-    constexpr int KT = 64 / M, OT = D / M, NP = KT * R, ROWS = M * kAttnWaves, LD = D + 4;
+    constexpr int KT = 64 / M, OT = D / M, NP = KT * R, W = M * NT, ROWS = W * kAttnWaves, LD = D + 4;
     constexpr int QS = D / (512 / M); // matrix instructions that a key tile's scores take (8 channels a lane each)
     typedef typename Mfma<M>::acc acc_t;
     __shared__ int found[5];
-    constexpr bool SHARED = D == 128 && M == 32;  // four wavefronts with rows of their own share the conversion of the codes
+    constexpr bool SHARED = D == 128 && M == 32 && NT == 1;  // four wavefronts with rows of their own share the conversion of the codes
     constexpr int HALF = 64 * D * 2;              // bytes of a block of K, or V, in binary16
-    static_assert(!SHARED || 4 * HALF <= (int)sizeof(float) * kAttnWaves * M * LD, "two stages of K and V fit");
-    __shared__ __attribute__((aligned(1024))) float acc_lds[kAttnWaves * M * LD];
-    __shared__ float2 ml_lds[kAttnWaves * M];
+    static_assert(!SHARED || 4 * HALF <= (int)sizeof(float) * kAttnWaves * W * LD, "two stages of K and V fit");
+    __shared__ __attribute__((aligned(1024))) float acc_lds[kAttnWaves * W * LD];
+    __shared__ float2 ml_lds[kAttnWaves * W];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lq = lane % M, g = lane / M;
     const int kvh = (int)blockIdx.x % a.Hkv, slot_x = (int)blockIdx.x / a.Hkv, split = blockIdx.y;
     Work wk;
@@ -150,10 +150,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     const int cap = a.pt.width * a.pt.page_tokens, true_len = max(wk.len, 0), len = min(true_len, cap);
 
     // ---- this wavefront's rows and blocks ----
-    const int RW = rows > 2 * M ? 4 : rows > M ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
+    const int RW = rows > 2 * W ? 4 : rows > W ? 2 : 1, KW = kAttnWaves / RW;  // row groups, key groups
     const int rg = wave % RW, kg = wave / RW;
-    const int first = tile * ROWS + rg * M;         // packed row of this wavefront's first
-    const int mine = min(rows - rg * M, M);         // rows of this wavefront, may be <= 0
+    const int first = tile * ROWS + rg * W;         // packed row of this wavefront's first
+    const int mine = min(rows - rg * W, W);         // rows of this wavefront, may be <= 0
     // the last key that packed row ri sees
     const auto last_key = [&](int ri) { return a.causal ? min(len - 1, len - n + ri / a.group) : len - 1; };
     const int lim_lo = last_key(first), lim_hi = mine > 0 ? last_key(first + mine - 1) : -1;
@@ -161,19 +161,26 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     if (split + 1 < a.splits) je = min(je, jb + a.split_blocks);
 
     // ---- Q: run i of 8 channels a lane ----
-    v8h qh[QS];
-    float row_scale;
-    const int ri0 = min(first + min(lq, max(mine, 1) - 1), n * a.group - 1);
-    const int lim = last_key(ri0);
-    const auto load_q = [&](uint4 (&qx)[QS]) {
-        const int tok = ri0 / a.group, hq = kvh * a.group + ri0 % a.group;
-        const uint16_t *p = a.q + (int64_t)(q0 + tok) * a.q_st.t + hq * a.q_st.h + 16 * g;
+    v8h qh[NT][QS];
+    float row_scale[NT];
+    int ri0[NT], lim[NT];
 #pragma unroll
-        for (int i = 0; i < QS; ++i) qx[i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
+    for (int n_ = 0; n_ < NT; ++n_) {
+        ri0[n_] = min(first + min(M * n_ + lq, max(mine, 1) - 1), n * a.group - 1);
+        lim[n_] = last_key(ri0[n_]);
+    }
+    const auto load_q = [&](uint4 (&qx)[NT][QS]) {
+#pragma unroll
+        for (int n_ = 0; n_ < NT; ++n_) {
+            const int tok = ri0[n_] / a.group, hq = kvh * a.group + ri0[n_] % a.group;
+            const uint16_t *p = a.q + (int64_t)(q0 + tok) * a.q_st.t + hq * a.q_st.h + 16 * g;
+#pragma unroll
+            for (int i = 0; i < QS; ++i) qx[n_][i] = *reinterpret_cast<const uint4 *>(p + (i >> 1) * (1024 / M) + 8 * (i & 1));
+        }
     };
-    const auto convert_q = [&](const uint4 (&qx)[QS]) {
+    const auto convert_rows = [&](const uint4 (&qx)[QS], v8h (&to)[QS], float &scale) {
         float s = 1.0f;
-        row_scale = a.scale;
+        scale = a.scale;
         if constexpr (BF16) {
             // binary16 has bfloat16's precision and more, not its range: the row is brought to 1 .. 2 by a power of two
             // (magnitudes in order of their bits, two at a time)
@@ -187,7 +194,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
             const float top = Mfma<M>::row_max(__builtin_bit_cast(float, (uint32_t)max(m2[0], m2[1]) << 16));
             const int ex = min(max((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127, -126), 126);
             s = __builtin_bit_cast(float, (uint32_t)(127 - ex) << 23);
-            row_scale *= __builtin_bit_cast(float, (uint32_t)(127 + ex) << 23);
+            scale *= __builtin_bit_cast(float, (uint32_t)(127 + ex) << 23);
         }
 #pragma unroll
         for (int i = 0; i < QS; ++i) {
@@ -196,14 +203,20 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
                 unpack8<true>(qx[i], f);
                 const uint4 w = make_uint4(pack_half(f[0] * s, f[1] * s), pack_half(f[2] * s, f[3] * s),
                                            pack_half(f[4] * s, f[5] * s), pack_half(f[6] * s, f[7] * s));
-                qh[i] = __builtin_bit_cast(v8h, w);
+                to[i] = __builtin_bit_cast(v8h, w);
             } else {
-                qh[i] = __builtin_bit_cast(v8h, qx[i]);
+                to[i] = __builtin_bit_cast(v8h, qx[i]);
             }
         }
     };
-    float m = -INFINITY, l = 0.0f, vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
-    acc_t o[OT];
+    const auto convert_q = [&](const uint4 (&qx)[NT][QS]) {
+#pragma unroll
+        for (int n_ = 0; n_ < NT; ++n_) convert_rows(qx[n_], qh[n_], row_scale[n_]);
+    };
+    float m[NT], l[NT], vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
+    acc_t o[NT][OT];
+#pragma unroll
+    for (int n_ = 0; n_ < NT; ++n_) m[n_] = -INFINITY, l[n_] = 0.0f;
 
     // ---- the keys, block by block ----
     // the place of the block that is fetched next: page number `at_page` of the slot, block `at_block` of it; a step of KW blocks is
@@ -241,64 +254,73 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         vs = there ? scalar_load(a.v_scale + blk) : __builtin_nanf("");
     };
 
-    v8h pb[NP / 8];
-    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far; MASKED: some row does not see
-    // some key of the block.
-    const auto softmax = [&](auto masked_c, acc_t (&s)[KT], int key0) {
+    v8h pb[NT][NP / 8];
+    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far, and f, what o is to be
+    // multiplied by; MASKED: some row does not see some key of the block.
+    const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0, float (&f)[NT]) {
         constexpr bool MASKED = decltype(masked_c)::value;
-        const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim; };
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int i = 0; i < R; ++i) s[t][i] = hidden(t, i) ? -INFINITY : s[t][i];
-        }
-        const float c = row_scale * ks;  // >= 0, so the order of the scores is that of the sums
-        float top = s[0][0];
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int i = 0; i < R; ++i) top = fmaxf(top, s[t][i]);
-        const float m_new = fmaxf(m, Mfma<M>::row_max(top) * c);
-        const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
-        const float alpha = __builtin_amdgcn_exp2f(m - base);
         // V's scale goes into the exponent (a block of zeros: any will do)
         const float vnew = fmaxf(vref, vs), back = vnew > vref ? vref * __builtin_amdgcn_rcpf(vnew) : 1.0f;
         const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
-        const float shift = (vs == vs ? lr : vs) - base;
-        float sum = 0.0f;
+        const float fold = vs == vs ? lr : vs, unfold = __builtin_amdgcn_exp2f(-lr);
 #pragma unroll
-        for (int st = 0; st < NP / 8; ++st) {
-            float p[8];
+        for (int n_ = 0; n_ < NT; ++n_) {
+            const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim[n_]; };
+            if constexpr (MASKED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = (8 * st + e) / R, i = (8 * st + e) % R;
-                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, shift));
-                if constexpr (MASKED) p[e] = hidden(t, i) ? 0.0f : p[e];  // (and no NaN of the scales comes in)
-                sum += p[e];
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int i = 0; i < R; ++i) s[n_][t][i] = hidden(t, i) ? -INFINITY : s[n_][t][i];
             }
-            const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
-            pb[st] = __builtin_bit_cast(v8h, w);
+            const float c = row_scale[n_] * ks;  // >= 0, so the order of the scores is that of the sums
+            float top = s[n_][0][0];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < R; ++i) top = fmaxf(top, s[n_][t][i]);
+            const float m_new = fmaxf(m[n_], Mfma<M>::row_max(top) * c);
+            const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
+            const float alpha = __builtin_amdgcn_exp2f(m[n_] - base);
+            const float shift = fold - base;
+            float sum = 0.0f;
+#pragma unroll
+            for (int st = 0; st < NP / 8; ++st) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = (8 * st + e) / R, i = (8 * st + e) % R;
+                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n_][t][i], c, shift));
+                    if constexpr (MASKED) p[e] = hidden(t, i) ? 0.0f : p[e];  // (and no NaN of the scales comes in)
+                    sum += p[e];
+                }
+                const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
+                pb[n_][st] = __builtin_bit_cast(v8h, w);
+            }
+            l[n_] = l[n_] * alpha + sum * unfold;
+            m[n_] = m_new;
+            f[n_] = alpha * back;
         }
-        l = l * alpha + sum * __builtin_amdgcn_exp2f(-lr);
-        m = m_new;
         vref = vnew;
-        return alpha * back;  // what o is to be multiplied by
     };
 
     const auto advance = [&]() {
         at_page += step_pages, at_block += step_blocks;
         if (at_block >= per_page) at_block -= per_page, ++at_page;
     };
-    const auto rescale = [&](float f) {  // where a maximum moved
-        if (__builtin_amdgcn_ballot_w64(f != 1.0f) != 0) {
+    const auto rescale = [&](const float (&f)[NT]) {  // where a maximum moved
 #pragma unroll
-            for (int i = 0; i < OT; ++i) o[i] *= f;
+        for (int n_ = 0; n_ < NT; ++n_) {
+            if (__builtin_amdgcn_ballot_w64(f[n_] != 1.0f) != 0) {
+#pragma unroll
+                for (int i = 0; i < OT; ++i) o[n_][i] *= f[n_];
+            }
         }
     };
     const auto clear = [&]() {
 #pragma unroll
-        for (int i = 0; i < OT; ++i) o[i] = acc_t{};
+        for (int n_ = 0; n_ < NT; ++n_)
+#pragma unroll
+            for (int i = 0; i < OT; ++i) o[n_][i] = acc_t{};
     };
     const auto masked = [&](int j) { return j * kBlock + kBlock - 1 > lim_lo; };
     // (the table is asked before the length is known, and the first block is on its way before Q is waited for)
@@ -306,7 +328,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
     // each wavefront on its own
     const auto alone = [&]() {
         asm volatile("" ::: "memory");  // (Q's loads stay on this side of the choice: in front of it they would be kept over the other loop)
-        uint4 qx[QS];
+        uint4 qx[NT][QS];
         load_q(qx);
         jb += kg;
         if (jb < je) {
@@ -323,31 +345,43 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
             if (j + KW < je) advance();  // (the last one fetches its own block again: no branch around the loads)
             size_t nblk;
             const bool there = block_here(nblk);
-            acc_t s[KT];
+            acc_t s[NT][KT];
+            // (an operand of K or V, converted once, meets all the wavefront's rows)
+            const auto scores_of = [&](v8h x, int t, int i) {
+#pragma unroll
+                for (int n_ = 0; n_ < NT; ++n_) s[n_][t] = Mfma<M>::run(x, qh[n_][i], i == 0 ? acc_t{} : s[n_][t]);
+            };
+            const auto sums_of = [&](v8h x, int t, int i) {
+#pragma unroll
+                for (int n_ = 0; n_ < NT; ++n_) o[n_][t] = Mfma<M>::run(x, pb[n_][i], o[n_][t]);
+            };
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < QS / 2; ++i) {
                     const uint4 x = kx[t * (QS / 2) + i];
-                    s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), qh[2 * i], i == 0 ? acc_t{} : s[t]);
-                    s[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), qh[2 * i + 1], s[t]);
+                    scores_of(codes_to_half<E4M3>(x.x, x.y), t, 2 * i);
+                    scores_of(codes_to_half<E4M3>(x.z, x.w), t, 2 * i + 1);
                     if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
                 }
             load_k(nblk);
-            rescale(masked(j) ? softmax(std::true_type{}, s, j * kBlock) : softmax(std::false_type{}, s, 0));
+            float f[NT];
+            if (masked(j)) softmax(std::true_type{}, s, j * kBlock, f);
+            else softmax(std::false_type{}, s, 0, f);
+            rescale(f);
             // O^T += V^T P^T
 #pragma unroll
             for (int t = 0; t < OT; ++t) {
                 if constexpr (M == 16) {
                     const uint4 x = vx[t];
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, x.y), pb[0], o[t]);
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, x.w), pb[1], o[t]);
+                    sums_of(codes_to_half<E4M3>(x.x, x.y), t, 0);
+                    sums_of(codes_to_half<E4M3>(x.z, x.w), t, 1);
                 } else {
                     const uint4 x = vx[2 * t], y = vx[2 * t + 1];
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.x, y.x), pb[0], o[t]);
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.y, y.y), pb[1], o[t]);
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.z, y.z), pb[2], o[t]);
-                    o[t] = Mfma<M>::run(codes_to_half<E4M3>(x.w, y.w), pb[3], o[t]);
+                    sums_of(codes_to_half<E4M3>(x.x, y.x), t, 0);
+                    sums_of(codes_to_half<E4M3>(x.y, y.y), t, 1);
+                    sums_of(codes_to_half<E4M3>(x.z, y.z), t, 2);
+                    sums_of(codes_to_half<E4M3>(x.w, y.w), t, 3);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -364,7 +398,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         // rate), INT8 / E4M3: each wavefront on its own 348 / 318 us, conversions shared 328 / 318, scores under the exponentials and operands
         // ahead 315 / 304, priority raised 302 / 294; matrix pipe 37 % and vector issue 48 % of the time, and little of the two overlaps.  At
         // d = 64, half the conversions, none of this is faster than a wavefront on its own (211 us; 208 to 215).
-        uint4 qx[QS];
+        uint4 qx[NT][QS];
         load_q(qx);
         uint8_t *stage = reinterpret_cast<uint8_t *>(acc_lds);
         constexpr int KN = NL / kAttnWaves;
@@ -404,7 +438,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         if (split + 1 < a.splits) je_all = min(je_all, jb + a.split_blocks);
         // Ahead of the block whose weights are computed: K by one (its scores are computed under the exponentials) and, in LDS, by two; V by one.
         float ks1 = 0.0f, vs1 = 0.0f, ks2 = 0.0f, vs2 = 0.0f;
-        acc_t s0[KT], s1[KT];
+        acc_t s0[NT][KT], s1[NT][KT];
         size_t vblk = blk;  // the block behind the one that is fetched
         const auto next_block = [&](int j) {  // (the last ones fetch a block again: no branch around the loads)
             vblk = blk;
@@ -413,23 +447,23 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
             ks2 = there ? scalar_load(a.k_scale + blk) : __builtin_nanf("");
             vs2 = there ? scalar_load(a.v_scale + blk) : __builtin_nanf("");
         };
-        const auto scores = [&](acc_t (&s)[KT], int buf) {
+        const auto scores = [&](acc_t (&s)[NT][KT], int buf) {
             const v8h *p = reinterpret_cast<const v8h *>(stage + HALF * buf) + lane;
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int i = 0; i < QS; ++i) s[t] = Mfma<M>::run(p[64 * (t * QS + i)], qh[i], i == 0 ? acc_t{} : s[t]);
+                for (int i = 0; i < QS; ++i) s[0][t] = Mfma<M>::run(p[64 * (t * QS + i)], qh[0][i], i == 0 ? acc_t{} : s[0][t]);
         };
         // block j: its scores are in `now`; the next one's go to `then`
-        const auto step = [&](int j, acc_t (&now)[KT], acc_t (&then)[KT], auto buf_c) {
+        const auto step = [&](int j, acc_t (&now)[NT][KT], acc_t (&then)[NT][KT], auto buf_c) {
             constexpr int BUF = decltype(buf_c)::value;
             if (j < je) {
-                float f;
+                float f[NT];
                 const auto both = [&](auto masked_c) {
                     __builtin_amdgcn_s_setprio(1);
                     __builtin_amdgcn_sched_barrier(0);
                     scores(then, BUF ^ 1);
-                    f = softmax(masked_c, now, j * kBlock);
+                    softmax(masked_c, now, j * kBlock, f);
                     // a matrix instruction, an operand four ahead, and what the vector unit does meanwhile
                     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -449,7 +483,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
 #pragma unroll
                 for (int t = 0; t < OT; ++t)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) o[t] = Mfma<M>::run(p[64 * (4 * t + w)], pb[w], o[t]);
+                    for (int w = 0; w < 4; ++w) o[0][t] = Mfma<M>::run(p[64 * (4 * t + w)], pb[0][w], o[0][t]);
                 __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
                 for (int i = 0; i < 4 * OT; ++i) {
@@ -499,44 +533,49 @@ __global__ __launch_bounds__(64 * kAttnWaves, M == 16 ? 3 : 2) void paged_rows_k
         alone();
     }
     // a length beyond the table's row: what the row cannot hold is missing
-    const float sum = Mfma<M>::row_sum(l) + (true_len > cap ? __builtin_nanf("") : 0.0f);
+    float sum[NT];
+#pragma unroll
+    for (int n_ = 0; n_ < NT; ++n_) sum[n_] = Mfma<M>::row_sum(l[n_]) + (true_len > cap ? __builtin_nanf("") : 0.0f);
 
     // ---- the key groups' sums ----
     const PagedArgs z = arguments_again();
+    const auto sums_at = [&](int n_, int t, int i) {
+        return make_float4(o[n_][t][i] * vref, o[n_][t][i + 1] * vref, o[n_][t][i + 2] * vref, o[n_][t][i + 3] * vref);
+    };
     if (KW == 1) {
-        if (lq >= mine) return;
-        const int ri = first + lq, tok = q0 + ri / z.group, hq = kvh * z.group + ri % z.group;
 #pragma unroll
-        for (int t = 0; t < OT; ++t)
+        for (int n_ = 0; n_ < NT; ++n_) {
+            if (M * n_ + lq >= mine) return;
+            const int ri = first + M * n_ + lq, tok = q0 + ri / z.group, hq = kvh * z.group + ri % z.group;
 #pragma unroll
-            for (int i = 0; i < R; i += 4)
-                store_sums<D, BF16>(z, tok, hq, M * t + 2 * i + 4 * g,
-                                    make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref), m, sum, split);
+            for (int t = 0; t < OT; ++t)
+#pragma unroll
+                for (int i = 0; i < R; i += 4) store_sums<D, BF16>(z, tok, hq, M * t + 2 * i + 4 * g, sums_at(n_, t, i), m[n_], sum[n_], split);
+        }
         return;
     }
-    {
-        const int r = wave * M + lq;
-        if (g == 0) ml_lds[r] = make_float2(m, sum);
+#pragma unroll
+    for (int n_ = 0; n_ < NT; ++n_) {
+        const int r = wave * W + M * n_ + lq;
+        if (g == 0) ml_lds[r] = make_float2(m[n_], sum[n_]);
 #pragma unroll
         for (int t = 0; t < OT; ++t)
 #pragma unroll
-            for (int i = 0; i < R; i += 4)
-                *reinterpret_cast<float4 *>(acc_lds + r * LD + M * t + 2 * i + 4 * g) =
-                    make_float4(o[t][i] * vref, o[t][i + 1] * vref, o[t][i + 2] * vref, o[t][i + 3] * vref);
+            for (int i = 0; i < R; i += 4) *reinterpret_cast<float4 *>(acc_lds + r * LD + M * t + 2 * i + 4 * g) = sums_at(n_, t, i);
     }
     __syncthreads();
     for (int e = tid; e < rows * (D / 4); e += 64 * kAttnWaves) {
-        const int r = e / (D / 4), ch = 4 * (e % (D / 4)), w0 = r / M, rr = r % M;
+        const int r = e / (D / 4), ch = 4 * (e % (D / 4)), w0 = r / W, rr = r % W;
         const int ri = tile * ROWS + r, tok = q0 + ri / z.group, hq = kvh * z.group + ri % z.group;
         float mx = -INFINITY;
-        for (int w = w0; w < kAttnWaves; w += RW) mx = fmaxf(mx, ml_lds[w * M + rr].x);
+        for (int w = w0; w < kAttnWaves; w += RW) mx = fmaxf(mx, ml_lds[w * W + rr].x);
         const float base = mx == -INFINITY ? 0.0f : mx;
         float all = 0.0f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = w0; w < kAttnWaves; w += RW) {
-            const float2 ml = ml_lds[w * M + rr];
+            const float2 ml = ml_lds[w * W + rr];
             const float f = __builtin_amdgcn_exp2f(ml.x - base);
-            const float4 y = *reinterpret_cast<const float4 *>(acc_lds + (w * M + rr) * LD + ch);
+            const float4 y = *reinterpret_cast<const float4 *>(acc_lds + (w * W + rr) * LD + ch);
             all += f * ml.y;
             acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
         }
@@ -633,14 +672,23 @@ void launch_merge(dim3 grid, hipStream_t stream, const PagedArgs &a) {
 }
 
 template <int D, bool BF16, bool E4M3>
-void launch_rows(int m, dim3 grid, hipStream_t stream, const PagedArgs &a) {
+void launch_rows(int w, dim3 grid, hipStream_t stream, const PagedArgs &a) {
     const dim3 block(64 * kAttnWaves);
-    if (m == 16) paged_rows_kernel<D, BF16, E4M3, 16><<<grid, block, 0, stream>>>(a);
-    else paged_rows_kernel<D, BF16, E4M3, 32><<<grid, block, 0, stream>>>(a);
+    if (w == 16) paged_rows_kernel<D, BF16, E4M3, 16, 1><<<grid, block, 0, stream>>>(a);
+    else if (w == 32) paged_rows_kernel<D, BF16, E4M3, 32, 1><<<grid, block, 0, stream>>>(a);
+    else if constexpr (D == 64) paged_rows_kernel<D, BF16, E4M3, 16, 3><<<grid, block, 0, stream>>>(a);
 }
 
-// Rows per wavefront, from the mean number of packed rows per sequence and K/V head.
-int wave_rows(int T, int B, int group) { return (int64_t)T * group <= 16 * (int64_t)B ? 16 : 32; }
+// Rows per wavefront, from the mean number of packed rows per sequence and K/V head.  A workgroup has 1, 2 or 4 groups of rows, so 33 to 48
+// rows would take two of 32 and 65 to 96 four; at d = 64 a wavefront has the registers for 48, which takes half as many and converts the codes half as
+// often (us, at 32 and 48 rows: 4 sequences x 40 rows x 20000 to 32768 tokens x 4 heads 26.1 and 23.8, 8 x 48 x 8192 to 16384 x 8 39.9 and
+// 33.8, 8 x 96 63.9 and 54.1; where it does not save a group it is slower: 8 x 64 40.7 and 51.2, 4 x 4096 x 4096 x 8 187 and 204.  64 rows
+// spill: 187 and 237).
+int wave_rows(int T, int B, int group, int d) {
+    const int64_t rows = (int64_t)T * group, each = B;
+    if (rows <= 16 * each) return 16;
+    return d == 64 && ((rows > 32 * each && rows <= 48 * each) || (rows > 64 * each && rows <= 96 * each)) ? 48 : 32;
+}
 int64_t row_slots(int T, int B, int group, int rows, bool ragged) {
     if (!ragged) return (int64_t)B * (((int64_t)(T / B) * group + rows - 1) / rows);
     return (int64_t)T * group / rows + B;
@@ -649,19 +697,21 @@ int64_t row_slots(int T, int B, int group, int rows, bool ragged) {
 }  // namespace
 
 int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
-    const int group = Hq / Hkv, rows = kAttnWaves * wave_rows(T, B, group);
+    const int group = Hq / Hkv, rows = kAttnWaves * wave_rows(T, B, group, 128);  // (one rule for both head dimensions)
     const int64_t tiles = ((int64_t)T * group + rows * (int64_t)B - 1) / (rows * (int64_t)B);  // of a sequence, at the mean
     const int64_t workgroups = tiles * B * Hkv;
     const int64_t blocks = cdiv(max_len, kBlock);
-    // Few workgroups: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than their
-    // wavefronts hide -- and none up to twelve blocks, where the second launch costs more than it saves (32 heads over 8, one sequence, us: 768
-    // tokens 8.5 in one range and 8.9 in three at d 128, 7.0 and 8.0 at d 64; 1280 tokens 10.6 and 9.7, 8.7 and 8.7).  Many: with 16 rows up to
-    // four per CU, since sequences of different lengths leave CUs idle, of 32 blocks at least (48 sequences of 1000 to 8192 tokens, d 128: one
-    // range 102, two 96, four 96, eight 96, sixteen 103); with 32 rows two, which is what a CU holds (six sequences, up to 512 rows over up to
-    // 16384 tokens: one range 454, two 284, four 305, eight 342).
-    int64_t ranges;
-    if (workgroups < kCUs) ranges = blocks <= 12 ? 1 : std::min((kCUs + workgroups / 2) / workgroups, blocks / 4);
-    else ranges = std::min(rows == 16 * kAttnWaves ? 4 * kCUs / workgroups : (2 * kCUs + workgroups / 2) / workgroups, blocks / 32);
+    // Fewer workgroups than CUs: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than
+    // their wavefronts hide -- and none up to twelve blocks, where the second launch costs more than it saves (32 heads over 8, one sequence, us: 768
+    // tokens 8.5 in one range and 8.9 in three at d 128, 7.0 and 8.0 at d 64; 1280 tokens 10.6 and 9.7, 8.7 and 8.7).
+    // Ranges of 32 blocks and more cost little, so there are more of them where sequences of different lengths would leave CUs idle: up to two
+    // per CU (16 rows, 24 sequences of 2000 to 16384 tokens, 8 heads, d 64: one range 67, two 51, all of 16384 tokens 75 and 78; 32 rows, d 64, 16
+    // sequences of 500 to 8192: one per CU 43, two 37; six of up to 512 rows over up to 16384 tokens, d 128: one range 454, two 284, four
+    // 305, eight 342); with 16 rows and no fewer workgroups than CUs up to four (48 sequences of 1000 to 8192 tokens, d 128: one range 102,
+    // two 96, four 96, eight 96, sixteen 103).
+    const int64_t one = blocks <= 12 ? 1 : std::min((kCUs + workgroups / 2) / workgroups, blocks / 4);
+    const int64_t two = rows > 16 * kAttnWaves ? (2 * kCUs + workgroups / 2) / workgroups : workgroups < kCUs ? 2 : 4 * kCUs / workgroups;
+    int64_t ranges = std::max(one, std::min(two, blocks / 32));
     ranges = std::max<int64_t>(1, ranges);
     // a multiple of four blocks: four wavefronts share a range's keys (1280 tokens, d 128: ranges of five blocks 9.8 us, of four 8.9)
     return (int)(((blocks + ranges - 1) / ranges + 3) / 4 * 4) * kBlock;
@@ -680,7 +730,7 @@ PagedScratch paged_scratch_layout(void *base, int T, int Hq, int d, int max_len,
 
 int64_t paged_attn_workgroups(int T, int B, int Hq, int Hkv, int d, bool ragged, int splits) {
     const int group = Hq / Hkv;
-    return Hkv * std::max(row_slots(T, B, group, kAttnWaves * wave_rows(T, B, group), ragged), splits > 1 ? row_slots(T, B, group, 1024 / d, ragged) : 0);
+    return Hkv * std::max(row_slots(T, B, group, kAttnWaves * wave_rows(T, B, group, d), ragged), splits > 1 ? row_slots(T, B, group, 1024 / d, ragged) : 0);
 }
 
 hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenStrides o_st, const sage_page_table &pt, const sage_cache &c,
@@ -689,14 +739,14 @@ hipError_t launch_paged_attn(const void *q, TokenStrides q_st, void *out, TokenS
     PagedArgs a{static_cast<const uint16_t *>(q), static_cast<uint16_t *>(out), q_st, o_st, pt, c.k, c.v, c.k_scale, c.v_scale, bt, Hq, c.Hkv,
                 Hq / c.Hkv, causal, split_keys / kBlock, ws.splits, (float)(sm_scale * 1.4426950408889634), ws.part_acc, ws.part_ml};
     const bool bf16 = c.dt == SAGE_BF16, e4m3 = c.fmt == SAGE_CACHE_E4M3;
-    const int m = wave_rows(bt.T, bt.B, a.group);
-    const dim3 grid((unsigned)(row_slots(bt.T, bt.B, a.group, kAttnWaves * m, bt.q_start != nullptr) * c.Hkv), (unsigned)ws.splits);
+    const int w = wave_rows(bt.T, bt.B, a.group, c.d);
+    const dim3 grid((unsigned)(row_slots(bt.T, bt.B, a.group, kAttnWaves * w, bt.q_start != nullptr) * c.Hkv), (unsigned)ws.splits);
     if (c.d == 128)
         (bf16 ? e4m3 ? launch_rows<128, true, true> : launch_rows<128, true, false>
-              : e4m3 ? launch_rows<128, false, true> : launch_rows<128, false, false>)(m, grid, stream, a);
+              : e4m3 ? launch_rows<128, false, true> : launch_rows<128, false, false>)(w, grid, stream, a);
     else
         (bf16 ? e4m3 ? launch_rows<64, true, true> : launch_rows<64, true, false>
-              : e4m3 ? launch_rows<64, false, true> : launch_rows<64, false, false>)(m, grid, stream, a);
+              : e4m3 ? launch_rows<64, false, true> : launch_rows<64, false, false>)(w, grid, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || ws.splits == 1) return e;
     const dim3 mgrid((unsigned)(row_slots(bt.T, bt.B, a.group, 1024 / c.d, bt.q_start != nullptr) * c.Hkv));

@@ -345,6 +345,15 @@ def test_long_chunks(fmt, dtype, causal):
         run_case(lens, [150, 200], Hq=6, Hkv=2, d=128, dtype=dtype, fmt=fmt, page=64, causal=causal, seed=21, split=split)
 
 
+@pytest.mark.parametrize("fmt,dtype", [("int8", "bf16"), ("e4m3", "fp16"), ("e4m3", "bf16"), ("int8", "fp16")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_between_the_tiles_of_32(fmt, dtype, causal):
+    # 33 to 48 and 65 to 96 packed rows on average, d 64: one, two and four groups of rows, two tiles, rows beyond a sequence's length
+    for lens, news, split in (([300, 5, 64], [5, 5, 5], 0), ([300, 129, 70, 515], [9, 1, 4, 8], 64), ([260, 1, 130, 64], [20, 1, 1, 1], 128),
+                              ([450, 12], [12, 12], 192), ([705, 64, 3, 65, 200], [44, 1, 1, 1, 1], 256), ([705, 40, 3, 65, 0], [44, 1, 1, 1, 1], 0)):
+        run_case(lens, news, Hq=16, Hkv=2, d=64, dtype=dtype, fmt=fmt, page=128, causal=causal, seed=sum(news), split=split)
+
+
 def test_rows_that_see_nothing_are_zeros():
     # more rows than tokens: the first ones lie in front of the sequence
     for split in (0, 64):
