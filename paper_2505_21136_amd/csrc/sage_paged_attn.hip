@@ -255,14 +255,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
     };
 
     v8h pb[NT][NP / 8];
-    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far, and f, what o is to be
-    // multiplied by; MASKED: some row does not see some key of the block.
-    const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0, float (&f)[NT]) {
+    struct Factors {
+        float of[NT];
+    };
+    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far; returns what o is to be
+    // multiplied by.  MASKED: some row does not see some key of the block.
+    const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0) {
         constexpr bool MASKED = decltype(masked_c)::value;
-        // V's scale goes into the exponent (a block of zeros: any will do)
-        const float vnew = fmaxf(vref, vs), back = vnew > vref ? vref * __builtin_amdgcn_rcpf(vnew) : 1.0f;
-        const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
-        const float fold = vs == vs ? lr : vs, unfold = __builtin_amdgcn_exp2f(-lr);
+        Factors f;
 #pragma unroll
         for (int n_ = 0; n_ < NT; ++n_) {
             const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim[n_]; };
@@ -281,7 +281,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
             const float m_new = fmaxf(m[n_], Mfma<M>::row_max(top) * c);
             const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
             const float alpha = __builtin_amdgcn_exp2f(m[n_] - base);
-            const float shift = fold - base;
+            // V's scale goes into the exponent (a block of zeros: any will do)
+            const float vnew = fmaxf(vref, vs), back = vnew > vref ? vref * __builtin_amdgcn_rcpf(vnew) : 1.0f;
+            const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
+            const float shift = (vs == vs ? lr : vs) - base;
             float sum = 0.0f;
 #pragma unroll
             for (int st = 0; st < NP / 8; ++st) {
@@ -296,23 +299,24 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                 const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
                 pb[n_][st] = __builtin_bit_cast(v8h, w);
             }
-            l[n_] = l[n_] * alpha + sum * unfold;
+            l[n_] = l[n_] * alpha + sum * __builtin_amdgcn_exp2f(-lr);
             m[n_] = m_new;
-            f[n_] = alpha * back;
+            f.of[n_] = alpha * back;
         }
-        vref = vnew;
+        vref = fmaxf(vref, vs);
+        return f;
     };
 
     const auto advance = [&]() {
         at_page += step_pages, at_block += step_blocks;
         if (at_block >= per_page) at_block -= per_page, ++at_page;
     };
-    const auto rescale = [&](const float (&f)[NT]) {  // where a maximum moved
+    const auto rescale = [&](const Factors &f) {  // where a maximum moved
 #pragma unroll
         for (int n_ = 0; n_ < NT; ++n_) {
-            if (__builtin_amdgcn_ballot_w64(f[n_] != 1.0f) != 0) {
+            if (__builtin_amdgcn_ballot_w64(f.of[n_] != 1.0f) != 0) {
 #pragma unroll
-                for (int i = 0; i < OT; ++i) o[n_][i] *= f[n_];
+                for (int i = 0; i < OT; ++i) o[n_][i] *= f.of[n_];
             }
         }
     };
@@ -365,10 +369,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                     if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
                 }
             load_k(nblk);
-            float f[NT];
-            if (masked(j)) softmax(std::true_type{}, s, j * kBlock, f);
-            else softmax(std::false_type{}, s, 0, f);
-            rescale(f);
+            rescale(masked(j) ? softmax(std::true_type{}, s, j * kBlock) : softmax(std::false_type{}, s, 0));
             // O^T += V^T P^T
 #pragma unroll
             for (int t = 0; t < OT; ++t) {
@@ -458,12 +459,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
         const auto step = [&](int j, acc_t (&now)[NT][KT], acc_t (&then)[NT][KT], auto buf_c) {
             constexpr int BUF = decltype(buf_c)::value;
             if (j < je) {
-                float f[NT];
+                Factors f;
                 const auto both = [&](auto masked_c) {
                     __builtin_amdgcn_s_setprio(1);
                     __builtin_amdgcn_sched_barrier(0);
                     scores(then, BUF ^ 1);
-                    softmax(masked_c, now, j * kBlock, f);
+                    f = softmax(masked_c, now, j * kBlock);
                     // a matrix instruction, an operand four ahead, and what the vector unit does meanwhile
                     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll

@@ -126,7 +126,7 @@ def sage_rope(q: torch.Tensor, positions: torch.Tensor, plan: _RopePlan, *, k: t
     qs, (T, Hq, d), Hkv = _rows(q, "q"), q.shape, 0
     qos = ks = kos = None
     if out is None:
-        out = q.new_empty((T, Hq, d))
+        out = torch.empty_like(q) if qs is None else q.new_empty((T, Hq, d))
     else:
         qos = _rows(out, "out")
         if out.shape != q.shape or out.dtype != q.dtype:
@@ -136,7 +136,7 @@ def sage_rope(q: torch.Tensor, positions: torch.Tensor, plan: _RopePlan, *, k: t
         if k.shape != (T, Hkv, d) or k.dtype != q.dtype:
             raise _sage.SageError("k must be [T, Hkv, d] of q's dtype")
         if k_out is None:
-            k_out = k.new_empty((T, Hkv, d))
+            k_out = torch.empty_like(k) if ks is None else k.new_empty((T, Hkv, d))
         else:
             kos = _rows(k_out, "k_out")
             if k_out.shape != k.shape or k_out.dtype != k.dtype:
@@ -277,7 +277,7 @@ def sage_attn_fwd_paged(q: torch.Tensor, cache: PagedCache, *, causal: bool, max
     T, Hq, d = q.shape
     os_ = None
     if out is None:
-        out = q.new_empty((T, Hq, d))
+        out = torch.empty_like(q) if qs is None else q.new_empty((T, Hq, d))
     else:
         os_ = _of_cache(out, cache, "out")
         if out.shape != q.shape:
