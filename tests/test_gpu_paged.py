@@ -354,6 +354,19 @@ def test_rows_between_the_tiles_of_32(fmt, dtype, causal):
         run_case(lens, news, Hq=16, Hkv=2, d=64, dtype=dtype, fmt=fmt, page=128, causal=causal, seed=sum(news), split=split)
 
 
+@pytest.mark.parametrize("d,rows,split", [(128, 1, 0), (128, 40, 256), (64, 3, 64), (64, 10, 0)])
+def test_large_values(d, rows, split):
+    # V of 2^127 / (number of keys) and a scale of its own per block, equal weights: no sum passes the range
+    n, Hkv = 1024, 2
+    cache = make_cache([n], Hkv=Hkv, d=d, dtype=torch.bfloat16, fmt="int8", page_tokens=64, seed=d)
+    v = sequence(cache, "v", 0, n)
+    cache.v_scale.mul_(2.0 ** 116 / float(v.abs().max()))
+    q = (torch.randn(rows, 8, d, generator=torch.Generator().manual_seed(3)) * 2.0 ** -60).bfloat16()
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=False, max_len=n, split_keys=split)
+    want, err = attention(q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), causal=False)
+    assert_attention(out, want, err, torch.bfloat16, f"{rows} rows")
+
+
 def test_rows_that_see_nothing_are_zeros():
     # more rows than tokens: the first ones lie in front of the sequence
     for split in (0, 64):
