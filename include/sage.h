@@ -414,7 +414,8 @@ typedef struct {
 /* The T rows of a call belong to B sequences: rows q_start[b] .. q_start[b+1]-1 (device int32 [B+1], ascending, within 0 .. T) to the
  * b-th, or T/B rows each where q_start is NULL (T a multiple of B).  Rows that belong to none are neither read nor written.
  * slots[b] (device int32 [B], or NULL for b itself, then B <= slots) is the sequence's slot; a sequence whose slot is outside the table
- * is padding: its rows are skipped too.  1 <= T, B <= 2^22, and T * Hq <= 2^30.  Sizes that would take a launch of more than 2^23
+ * is padding: its rows are skipped too.  With starts that are not ascending it is open what the rows get, but nothing behind the T rows is
+ * read or written.  1 <= T, B <= 2^22, and T * Hq <= 2^30.  Sizes that would take a launch of more than 2^23
  * workgroups in one dimension are refused (SAGE_EINVAL). */
 
 /* ---- rotary positions --------------------------------------------------- */

@@ -38,6 +38,7 @@ def sources():
     out.append(os.path.join(CSRC, "sage_attn_device.h"))
     out.append(os.path.join(CSRC, "sage_tile_copy.h"))
     out.append(os.path.join(CSRC, "sage_paged.h"))
+    out.append(os.path.join(CSRC, "sage_paged_rows.h"))
     out.append(os.path.join(os.path.dirname(HERE), "include", "sage.h"))
     return out
 

@@ -4,6 +4,7 @@
 #include "../../include/sage.h"
 #include "sage_attn_device.h"
 #include "sage_internal.h"
+#include "sage_paged_rows.h"
 
 namespace sage {
 
@@ -40,7 +41,8 @@ struct Work {
 // rows).  Uniform batches: by division.  Ragged ones: sequence b owns the tiles from
 // floor(q_start[b] * per / rows) + b on -- as many as it can need, since ceil(n p / r) <= floor((a + n) p / r) - floor(a p / r) + 1
 // -- and the threads of the workgroup look at all of them at once (one round of loads for up to blockDim.x sequences, where a search by
-// halves would wait for memory log2(B) times); the one that finds it fetches the length too.  Returns false for a tile that nobody needs
+// halves would wait for memory log2(B) times); the one that finds it fetches the length too.  (Starts that are not
+// ascending can let several find it: each of the five numbers is then one of theirs, and the rows are cut to the call's.)  Returns false for a tile that nobody needs
 // and for padding.  Has a barrier; `shared` holds five numbers.
 __device__ __forceinline__ bool locate(const Batch &bt, const sage_page_table &pt, int x, int rows, int per, Work &w, int *shared) {
     if (!bt.q_start) {
@@ -55,17 +57,16 @@ __device__ __forceinline__ bool locate(const Batch &bt, const sage_page_table &p
     if (threadIdx.x == 0) shared[2] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < bt.B; i += blockDim.x) {
-        const int q0 = min(max(bt.q_start[i], 0), bt.T), q1 = min(max(bt.q_start[i + 1], 0), bt.T);
+        const RowClaim c = row_claim(bt.q_start[i], bt.q_start[i + 1], i, bt.T, rows, per);
         const int slot = bt.slots ? bt.slots[i] : i;
-        const int first = (int)((int64_t)q0 * per / rows) + i, next = (int)((int64_t)q1 * per / rows) + i + 1;
-        if (x >= first && x < next && q1 > q0 && slot >= 0 && slot < pt.slots) {
+        if (claims(c, x) && slot >= 0 && slot < pt.slots) {
             const int len = pt.lens[slot];
-            shared[0] = x - first, shared[1] = q0, shared[2] = q1 - q0, shared[3] = slot, shared[4] = len;
+            shared[0] = x - c.first, shared[1] = c.q0, shared[2] = c.q1 - c.q0, shared[3] = slot, shared[4] = len;
         }
     }
     __syncthreads();
     const auto uniform = [&](int i) { return __builtin_amdgcn_readfirstlane(shared[i]); };
-    w.tile = uniform(0), w.q0 = uniform(1), w.n = uniform(2), w.slot = uniform(3), w.len = uniform(4);
+    w.tile = uniform(0), w.q0 = uniform(1), w.n = rows_left(w.q0, uniform(2), bt.T), w.slot = uniform(3), w.len = uniform(4);
     return w.n > 0;
 }
 

@@ -1,0 +1,32 @@
+"""The paged cache where calls meet what goes wrong in a serving program: lengths beyond the table's row, pages that two sequences share, V blocks of
+very different sizes, missing pages, starts that go back; and the sizes at which the kernels change their ways."""
+import math
+
+import pytest
+import torch
+
+import paper_2505_21136_amd as sage
+from paged_ref import EPS, Table, attention, byte_table, make_cache, sequence
+from test_gpu_paged import DEV, DTYPES, check_blocks, empty, ints, run_case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d,Hq", [(64, 2), (64, 32), (128, 16)])
+def test_starts_that_claim_the_same_tiles_stay_within_the_call(d, Hq):
+    """Row starts have to be ascending; with others it is open what a row gets, but nothing outside the call's rows is touched: sequences far enough
+    apart that different wavefronts find the same tile."""
+    dt, T, B = torch.float16, 640, 300
+    cache = make_cache([130] * B, Hkv=1, d=d, dtype=dt, fmt="int8", page_tokens=64, seed=2)
+    starts = ints(*[(0, T, 9, T - 4)[i % 4] for i in range(B + 1)])
+    q = torch.randn(2 * T, Hq, d, device=DEV).to(dt)
+    for split in (0, 64):
+        room = torch.full((2 * T, Hq, d), 9.0, device=DEV, dtype=dt)
+        sage.sage_attn_fwd_paged(q[:T], cache, causal=True, max_len=130, q_start=starts, out=room[:T], split_keys=split)
+        assert bool((room[T:] == 9).all()) and bool((room[:T] != 9).any())
+    room = torch.full((2, 2 * T, 1, d), 9.0, device=DEV, dtype=dt)
+    assert sage.lib().sage_paged_gather(cache.pages.ref, cache.ref, room[0].data_ptr(), room[1].data_ptr(), starts.data_ptr(), None, B, T,
+                                        torch.cuda.current_stream().cuda_stream) == 0
+    assert bool((room[:, T:] == 9).all()) and bool((room[:, :T] != 9).any())
+    sage.sage_paged_append(cache, q[:T, :1], q[:T, :1], q_start=starts)
+    torch.cuda.synchronize()
