@@ -474,7 +474,8 @@ int sage_rope(const void *q, void *q_out, const void *k, void *k_out, const int3
  *   k, v       device, [T, Hkv, d] of cache->dt through strides {token, head} as for sage_rope         (in)
  * A slot may appear once in a call.  Pages that hold the touched blocks must not be shared (sage_pages_fork sees to that, unless a
  * sequence is then shortened into a page that it shares).
- * Rows in front of the sequence's start (more rows than lens) and blocks without a page are not written.
+ * Rows in front of the sequence's start (more rows than lens), blocks without a page and sequences whose length is beyond the table's row
+ * are not written.
  */
 int sage_paged_append(const sage_page_table *pages, const sage_cache *cache, const void *k, const void *v, const int64_t *k_strides,
                       const int64_t *v_strides, const int32_t *q_start, const int32_t *slots, int B, int T, const sage_rope_plan *rope,

@@ -69,11 +69,13 @@ template <int D, bool BF16, bool E4M3, bool is_v>
 __device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_rope_plan &plan, const Work &wk, int h, float (&red)[2][2][4]) {
     constexpr int WAVES = 2 * D / 64;
     const int Hkv = a.c.Hkv;
-    const int q0 = wk.q0, n = wk.n, slot = wk.slot, len = min(wk.len, a.pt.width * a.pt.page_tokens);
+    const int q0 = wk.q0, n = wk.n, slot = wk.slot, len = wk.len;
+    // (a length that the table's row cannot hold says nothing about where the rows belong: none of them is written)
+    if (len <= 0 || len > a.pt.width * a.pt.page_tokens) return;
     const int start = max(len - n, 0);  // first new token; row q0 + p - (len - n) is token p
     const int row0 = q0 - (len - n);
     const int j0 = start / kBlock, jl = (len - 1) / kBlock;
-    if (len <= 0 || j0 + wk.tile > jl) return;
+    if (j0 + wk.tile > jl) return;
     const int x_end = (wk.tile + 1) * kBlock >= n ? jl - j0 : wk.tile;  // the last workgroup goes on to the last block
     const TokenStrides st = is_v ? a.v_st : a.k_st;
     const int tid = threadIdx.x;

@@ -30,3 +30,34 @@ def test_starts_that_claim_the_same_tiles_stay_within_the_call(d, Hq):
     assert bool((room[:, T:] == 9).all()) and bool((room[:, :T] != 9).any())
     sage.sage_paged_append(cache, q[:T, :1], q[:T, :1], q_start=starts)
     torch.cuda.synchronize()
+
+
+def _everything(pages, cache):
+    """Copies of all that an append may write."""
+    return [t.clone().view(torch.uint8) for t in (pages.table, pages.lens, pages.refs, cache.k, cache.v, cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)]
+
+
+@pytest.mark.parametrize("length", [129, 130, 200, 2 ** 31 - 1])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_a_length_beyond_the_row_appends_nothing(length, rotated):
+    """The row is full and its pages are there, so the tokens would have a place to go: the last of the row's, which other tokens have."""
+    d, Hkv, dt = 64, 2, torch.bfloat16
+    pages, cache = empty(2, Hkv, d, dt, "int8", 64, 2)
+    plan = sage.rope_plan(d) if rotated else None
+    k, v = (torch.randn(128 + 70 + 6, Hkv, d, device=DEV).to(dt) for _ in "kv")
+    sage.sage_pages_reserve(pages, ints(128, 70))
+    sage.sage_paged_append(cache, k[:198], v[:198], q_start=ints(0, 128, 198), rope=plan)
+    pages.lens[0] = length
+    sage.sage_pages_reserve(pages, ints(3), ints(1))
+    before = _everything(pages, cache)
+    sage.sage_paged_append(cache, k[198:201], v[198:201], q_start=ints(0, 3, 3), rope=plan)
+    for x, y in zip(before, _everything(pages, cache)):
+        assert torch.equal(x, y)
+    # another sequence of the same call gets its tokens
+    sage.sage_paged_append(cache, k[198:], v[198:], q_start=ints(0, 3, 6), rope=plan)
+    pages.lens[0] = 128
+    for slot, rows in ((0, list(range(128))), (1, list(range(128, 198)) + [201, 202, 203])):
+        kk = k[rows]
+        if rotated:
+            kk = sage.sage_rope(kk, torch.arange(len(rows), dtype=torch.int32, device=DEV), plan)
+        check_blocks(cache, slot, {"k": kk.cpu(), "v": v[rows].cpu()})
