@@ -150,9 +150,23 @@ def sage_rope(q: torch.Tensor, positions: torch.Tensor, plan: _RopePlan, *, k: t
     return out if k is None else (out, k_out)
 
 
-class PageTable:
+class _Handle:
+    """Attributes are set once: the calls go by the addresses and sizes that the handle was made with, and its tensors keep that memory alive.  What
+    the tensors hold is changed in place."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:
+            raise _sage.SageError(f"{type(self).__name__}.{name} is set when the handle is made: change a tensor in place (copy_, sub_, [...] =), "
+                                  "or make another handle")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise _sage.SageError(f"{type(self).__name__}.{name} belongs to the handle as long as it lives")
+
+
+class PageTable(_Handle):
     """Which pages belong to which slot: table int32 [slots, width] (-1: none), lens int32 [slots], refs int32 [n_pages].  The caches of all
-    layers share one."""
+    layers share one.  The tensors' values may be changed, in place (drafted tokens are taken back by ``pages.lens.sub_(n)``); the tensors stay."""
 
     def __init__(self, *, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, page_tokens: int):
         if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
@@ -172,7 +186,7 @@ class PageTable:
                    page_tokens=page_tokens)
 
 
-class PagedCache:
+class PagedCache(_Handle):
     """The 8-bit K/V cache of one layer: k, v uint8 [n_pages, Hkv, page_tokens / 64, 64 * d], k_scale, v_scale float32 [n_pages, Hkv,
     page_tokens / 64], k_tail, v_tail [slots, Hkv, 128, d] in 16 bits, k_shift float32 [Hkv, d] or None; fmt 'int8' or 'e4m3'."""
 
