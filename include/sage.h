@@ -472,10 +472,11 @@ int sage_rope(const void *q, void *q_out, const void *k, void *k_out, const int3
  * lens) to any length down to 64 tokens below the longest it has had, and goes on from there: drafted tokens are taken back so.  With
  * `rope`, K is rotated by its index in the sequence, and rounded to `dt`, on the way.
  *   k, v       device, [T, Hkv, d] of cache->dt through strides {token, head} as for sage_rope         (in)
- * A slot may appear once in a call.  Pages that hold the touched blocks must not be shared (sage_pages_fork sees to that, unless a
- * sequence is then shortened into a page that it shares).
+ * A slot may appear once in a call.
  * Rows in front of the sequence's start (more rows than lens), blocks without a page and sequences whose length is beyond the table's row
- * are not written.
+ * are not written; neither are blocks in pages that other slots name too (refs above 1), whose tokens stay.  sage_pages_fork gives
+ * every sequence a last page of its own; one that is shortened afterwards into a page that it shares is forked into an empty slot, which
+ * copies that page, before it goes on there (and its old slot freed): appended to where it is, it would go on reading the others' tokens.
  */
 int sage_paged_append(const sage_page_table *pages, const sage_cache *cache, const void *k, const void *v, const int64_t *k_strides,
                       const int64_t *v_strides, const int32_t *q_start, const int32_t *slots, int B, int T, const sage_rope_plan *rope,

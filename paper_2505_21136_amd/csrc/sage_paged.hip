@@ -156,6 +156,7 @@ __device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_ro
         const int j = j0 + x, p0 = j * kBlock;
         int in_page;
         const int per_page = a.pt.page_tokens / kBlock, page = page_of(a.pt, slot, j, per_page, in_page);
+        const int shares = page >= 0 ? scalar_load(a.pt.refs + page) : 0;  // slots that name the page
         load(p0);
         // ---- the largest value, and whether all are finite ----
         float amax = 0.0f, odd = 0.0f;
@@ -187,7 +188,7 @@ __device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_ro
         block_scale<E4M3>(amax, odd != 0.0f, scale, factor);
 
         // ---- codes and scale ----
-        if (page >= 0) {
+        if (page >= 0 && shares <= 1) {  // (a page of others too is theirs as well)
             const size_t blk = ((size_t)page * Hkv + h) * per_page + in_page;
             uint8_t *out = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
             if (tid == 0) (is_v ? a.c.v_scale : a.c.k_scale)[blk] = scale;

@@ -61,3 +61,37 @@ def test_a_length_beyond_the_row_appends_nothing(length, rotated):
         if rotated:
             kk = sage.sage_rope(kk, torch.arange(len(rows), dtype=torch.int32, device=DEV), plan)
         check_blocks(cache, slot, {"k": kk.cpu(), "v": v[rows].cpu()})
+
+
+@pytest.mark.parametrize("back", [1, 3, 64])
+def test_an_append_leaves_shared_pages_as_they_are(back):
+    """Two sequences share whole pages, one is shortened into them and goes on (back = 64: from a page's first token): the other one's tokens
+    stay.  Forked into a slot of its own first, the shortened one goes on as if it had been alone."""
+    d, Hkv, dt, n = 64, 2, torch.float16, 128
+    pages, cache = empty(4, Hkv, d, dt, "e4m3", 64, 4)
+    k, v = (torch.randn(n + 5, Hkv, d, device=DEV).to(dt) for _ in "kv")
+    sage.sage_pages_reserve(pages, ints(n), ints(0))
+    sage.sage_paged_append(cache, k[:n], v[:n], slots=ints(0))
+    status, moves, slot_moves = sage.sage_pages_fork(pages, ints(0, 0), ints(1, 2))
+    assert status.tolist() == [0, 0]
+    sage.sage_pages_copy(cache, moves, slot_moves)
+    both = {"k": k[:n].cpu(), "v": v[:n].cpu()}
+    pages.lens[1].sub_(back)
+    assert pages.table[1, :2].tolist() == pages.table[2, :2].tolist()
+    sage.sage_pages_reserve(pages, ints(5), ints(1))
+    sage.sage_paged_append(cache, k[n:], v[n:], slots=ints(1))
+    for slot in (0, 2):
+        check_blocks(cache, slot, both)
+    # slot 2 goes on after taking as many tokens back, by way of slot 3
+    pages.lens[2].sub_(back)
+    status, moves, slot_moves = sage.sage_pages_fork(pages, ints(2), ints(3))
+    assert status.tolist() == [0]
+    sage.sage_pages_copy(cache, moves, slot_moves)
+    sage.sage_pages_free(pages, ints(2))
+    sage.sage_pages_reserve(pages, ints(5), ints(3))
+    sage.sage_paged_append(cache, k[n:], v[n:], slots=ints(3))
+    check_blocks(cache, 0, both)
+    rows = list(range(n - back)) + list(range(n, n + 5))
+    check_blocks(cache, 3, {"k": k[rows].cpu(), "v": v[rows].cpu()}, shortened=True)
+    t = Table(pages)
+    assert t.count() == t.refs
