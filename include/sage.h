@@ -506,8 +506,10 @@ int sage_paged_gather(const sage_page_table *pages, const sage_cache *cache, voi
  *               it has to be initialised
  *   sm_scale    as for the other attention calls
  * Q K^T and P V run in 16-bit matrix instructions on the codes (exact in binary16; bfloat16 rows of Q are scaled by a power of two) with
- * binary32 sums; P~ is rounded to binary16 after the block's V scale, relative to the largest so far, is multiplied in; maximum, sum
- * and output are binary32, and the output is divided by the sum of the weights last: V up to 2^127 / (number of keys) in magnitude is safe.
+ * binary32 sums; P~ is rounded to binary16 after the block's V scale, over a power of two that follows the blocks' scales, is multiplied in: half
+ * a step (2^-11) off for weights down to 2^-20 of the row's largest so far, 2^-31 of the largest beyond.  Blocks whose V is 2^-60 and less of
+ * another block's lose precision.  Maximum, sum and output are binary32, and the output is divided by the sum of the weights last: V up to
+ * 2^127 / (number of keys) in magnitude is safe.
  */
 int sage_paged_split_keys(int T, int B, int Hq, int Hkv, int max_len);
 size_t sage_paged_workspace_bytes(int T, int B, int Hq, int Hkv, int d, int max_len, int split_keys);

@@ -1,8 +1,8 @@
 // Attention over the paged 8-bit cache (gfx950; not treated in the paper): rows of any number per sequence, one kernel.
 //
 // S^T = K Q^T and O^T = V^T P^T in 16-bit matrix instructions (16x16x32, 32x32x16) with binary32 accumulators; the codes of K and V become binary16
-// in registers, exactly.  The scales of a block of 64 keys are one number each for K and V: K's goes into the softmax's constant, V's, relative to
-// the largest so far, into P~ before it is rounded.  One pass over the keys with running maximum and sum.
+// in registers, exactly.  The scales of a block of 64 keys are one number each for K and V: K's goes into the softmax's constant, V's, over a power
+// of two near it, into P~ before it is rounded.  One pass over the keys with running maximum and sum.
 //
 // The cache keeps the bytes of a block in the order of the operands, so a wavefront loads 1 KB of neighbouring bytes at a time
 // straight into registers; nothing of K, V or P passes through LDS and the loop has no barrier (128 rows at d = 128 excepted, below).  The rows of all query heads that share a
@@ -30,6 +30,12 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = SAGE_CACHE_BLOCK, kAttnWaves = 4;
+// O stands in units of 2^(ref - kLift), where 2^ref is near the V scales of late; a block's scale over that unit goes into P~.  ref moves to a block's
+// own power of two where that is larger or kNear below: O is then multiplied by a power of two, exactly.  A weight p of a row (its largest
+// is 1) becomes p * 2^(kLift - kNear) .. p * 2^(kLift + 1), which binary16 holds with all its bits down to p = 2^-20 and not at all
+// only below 2^-31, whatever the scales of the blocks before.  It never falls more than kSpan below the largest so far, so that O stays finite: keys
+// whose V is 2^-kSpan of others' lose precision.
+constexpr int kLift = 14, kNear = 8, kSpan = 60, kNoRef = -512;
 
 struct PagedArgs {
     const uint16_t *q;
@@ -213,7 +219,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
 #pragma unroll
         for (int n_ = 0; n_ < NT; ++n_) convert_rows(qx[n_], qh[n_], row_scale[n_]);
     };
-    float m[NT], l[NT], vref = 0.0f;  // vref: the largest V scale so far; o stands for o * vref
+    float m[NT], l[NT];
+    int vexp = kNoRef, vtop = kNoRef;  // ref, and the largest that it would have been
     acc_t o[NT][OT];
 #pragma unroll
     for (int n_ = 0; n_ < NT; ++n_) m[n_] = -INFINITY, l[n_] = 0.0f;
@@ -258,11 +265,22 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
     struct Factors {
         float of[NT];
     };
-    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over the largest so far; returns what o is to be
+    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over o's unit; returns what o is to be
     // multiplied by.  MASKED: some row does not see some key of the block.
     const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0) {
         constexpr bool MASKED = decltype(masked_c)::value;
         Factors f;
+        // V's scale goes into the exponent: its power of two over the unit, and the logarithm of what is left, 1 .. 2 (a block of zeros: any will do)
+        const uint32_t vbits = __builtin_bit_cast(uint32_t, vs);
+        const int e = (int)(vbits >> 23) - 127;  // (128: not finite)
+        const bool counts = vs > 0.0f && e < 128;
+        vtop = counts ? max(vtop, e) : vtop;
+        const int ref = counts && (e > vexp || e < vexp - kNear) ? max(e, vtop - kSpan) : vexp, moved = vexp - ref;
+        const float back = moved < -126 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(127 + moved) << 23);
+        const float rest = __builtin_amdgcn_logf(__builtin_bit_cast(float, (vbits & 0x7fffffu) | 0x3f800000u));
+        const float lr = counts ? (float)max(e - ref, -kSpan) + (rest + kLift) : 0.0f;
+        const float unlift = __builtin_amdgcn_exp2f(-lr);
+        vexp = ref;
 #pragma unroll
         for (int n_ = 0; n_ < NT; ++n_) {
             const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim[n_]; };
@@ -281,10 +299,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
             const float m_new = fmaxf(m[n_], Mfma<M>::row_max(top) * c);
             const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
             const float alpha = __builtin_amdgcn_exp2f(m[n_] - base);
-            // V's scale goes into the exponent (a block of zeros: any will do)
-            const float vnew = fmaxf(vref, vs), back = vnew > vref ? vref * __builtin_amdgcn_rcpf(vnew) : 1.0f;
-            const float lr = vs == 0.0f ? 0.0f : fmaxf(__builtin_amdgcn_logf(vs) - __builtin_amdgcn_logf(vnew), -60.0f);
-            const float shift = (vs == vs ? lr : vs) - base;
+            const float shift = (e < 128 ? lr : __builtin_nanf("")) - base;
             float sum = 0.0f;
 #pragma unroll
             for (int st = 0; st < NP / 8; ++st) {
@@ -299,11 +314,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                 const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
                 pb[n_][st] = __builtin_bit_cast(v8h, w);
             }
-            l[n_] = l[n_] * alpha + sum * __builtin_amdgcn_exp2f(-lr);
+            l[n_] = l[n_] * alpha + sum * unlift;
             m[n_] = m_new;
             f.of[n_] = alpha * back;
         }
-        vref = fmaxf(vref, vs);
         return f;
     };
 
@@ -540,8 +554,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
 
     // ---- the key groups' sums ----
     const PagedArgs z = arguments_again();
+    const float unit = vexp < -112 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(127 + vexp - kLift) << 23);  // (below: nothing but zeros was seen)
     const auto sums_at = [&](int n_, int t, int i) {
-        return make_float4(o[n_][t][i] * vref, o[n_][t][i + 1] * vref, o[n_][t][i + 2] * vref, o[n_][t][i + 3] * vref);
+        return make_float4(o[n_][t][i] * unit, o[n_][t][i + 1] * unit, o[n_][t][i + 2] * unit, o[n_][t][i + 3] * unit);
     };
     if (KW == 1) {
 #pragma unroll

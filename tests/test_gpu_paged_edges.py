@@ -95,3 +95,79 @@ def test_an_append_leaves_shared_pages_as_they_are(back):
     check_blocks(cache, 3, {"k": k[rows].cpu(), "v": v[rows].cpu()}, shortened=True)
     t = Table(pages)
     assert t.count() == t.refs
+
+
+def _bounded_by_own_blocks(got, q, k, v, dtype, what, causal=True):
+    """Attention against 64 bits with a bound in which every key counts with its own V alone.
+
+    As paged_ref.attention's, with another last term: a weight's rounding to binary16 is 2^-11 of it or, where it is small, half the spacing of
+    the smallest numbers, 2^-25.  The weight is multiplied by 2^14 and by its block's V scale over a power of two that is at
+    most 2^8 times the scale, so that this is at most 2^-25 2^-14 2^8 = 2^-31 |v|, where the row's largest weight is 1 and the sum that all is
+    divided by at least 1 - 2^-20; nor more than the weight itself: min(p, 2^-30) |v| is granted."""
+    want, _ = attention(q, k, v, causal=causal)
+    n, Hq, d = q.shape
+    N, Hkv = k.shape[0], k.shape[1]
+    err = torch.zeros_like(want)
+    for h in range(Hq):
+        kk, vv = k[:, h * Hkv // Hq], v[:, h * Hkv // Hq]
+        s, big = q[:, h].double() @ kk.T / math.sqrt(d), q[:, h].double().abs() @ kk.abs().T / math.sqrt(d)
+        seen = torch.arange(N)[None] <= (torch.arange(n)[:, None] + N - n if causal else torch.full((n, 1), N))
+        s, big = s.masked_fill(~seen, -math.inf), big.masked_fill(~seen, 0.0)
+        p = torch.softmax(s, -1)
+        e = (d + 8) * 2.0 ** -24 * big.amax(-1, keepdim=True)
+        err[:, h] = (p @ vv.abs()) * (2 * (e + 2.0 ** -20) + 2.0 ** -11 + (N / 64 + 8) * 2.0 ** -23) + p.clamp(max=2.0 ** -30) @ vv.abs()
+    tol = err + EPS[dtype] * (want.abs() + err) + 2.0 ** -24
+    got = got.double().cpu()
+    assert torch.isfinite(got).all(), what
+    worst = ((got - want).abs() / tol).max().item()
+    print(f"   {what}: {worst:.3f} of the bound", flush=True)
+    assert worst <= 1.0, f"{what}: {worst:.3f} of the bound"
+
+
+# the packed rows of a sequence: one wavefront of 16, of 48 (d 64), of 32, rows of their own (d 64) and with shared conversions (d 128)
+ROWS = [(64, 1), (64, 12), (64, 40), (64, 8), (128, 1), (128, 8), (128, 40)]
+
+
+@pytest.mark.parametrize("d,rows", ROWS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("where", ["first", "middle", "in turn", "shrinking"])
+@pytest.mark.parametrize("ratio", [12, 16, 24])
+def test_blocks_of_large_v_take_no_precision_from_the_others(d, rows, dtype, where, ratio):
+    """Blocks with 2^ratio times the others' V and next to none of the weight: what the row gives the others comes out as it does without them."""
+    n, Hq, Hkv, dt, fmt = 64 * 18 - 9, 8, 2, DTYPES[dtype], "int8" if rows % 3 else "e4m3"
+    cache = make_cache([n], Hkv=Hkv, d=d, dtype=dt, fmt=fmt, page_tokens=64, seed=rows + d)
+    table = cache.pages.table[0].tolist()
+    loud = {"first": [0], "middle": [7, 8], "in turn": list(range(0, 17, 2)), "shrinking": range(0, 17)}[where]
+    cache.v_scale.clamp_(min=0.01, max=0.012)
+    cache.k_scale.clamp_(max=0.004 if fmt == "int8" else 0.0012)
+    # the first channel of K says how loud a block is: nothing else of it has any weight; q sees it with 2^6, so its keys lose 2^6 * 8 / sqrt(d) at least
+    where_k = byte_table("k", d)
+    none, low = (128, 0) if fmt == "int8" else (0, 0xfe)     # 0, and -128 or -448 times the scale
+    cache.k[:, :, 0, where_k[:, 0].to(DEV)] = none
+    for j in loud:
+        p = table[j]
+        if where == "shrinking":                             # each a little smaller than the one before; all that counts is in the last
+            cache.v_scale[p] *= 2.0 ** (ratio * (17 - j) / 17.0)
+        else:
+            cache.v_scale[p] *= 2.0 ** ratio
+        cache.k[p, :, 0, where_k[:, 0].to(DEV)] = low
+    q = torch.randn(rows, Hq, d, generator=torch.Generator().manual_seed(rows))
+    q[..., 0] = 512.0 if d == 64 else 700.0
+    q = q.to(dt)
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=True, max_len=n)
+    k, v = sequence(cache, "k", 0, n), sequence(cache, "v", 0, n)
+    _bounded_by_own_blocks(out, q, k, v, dt, f"{rows} rows")
+
+
+@pytest.mark.parametrize("d,rows", ROWS)
+@pytest.mark.parametrize("loud", [[0], [9], [17], [3, 11, 12]])
+def test_blocks_of_v_very_far_apart_stay_finite(d, rows, loud):
+    # equal weights: the large blocks are the result, and the sums of them pass by those that are 2^112 below
+    n, dt = 64 * 18 - 9, torch.bfloat16
+    cache = make_cache([n], Hkv=2, d=d, dtype=dt, fmt="int8", page_tokens=64, seed=rows)
+    cache.v_scale.fill_(0.01)
+    for j in loud:
+        cache.v_scale[int(cache.pages.table[0, j])] *= 2.0 ** 112
+    q = (torch.randn(rows, 8, d, generator=torch.Generator().manual_seed(rows)) * 2.0 ** -40).to(dt)
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=False, max_len=n)
+    _bounded_by_own_blocks(out, q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), dt, f"{rows} rows", causal=False)
