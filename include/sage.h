@@ -370,7 +370,8 @@ int sage_attn_fwd_decode(const void *q, const int8_t *k_i8, const uint8_t *v_fp8
  * Sequences live in SLOTS.  A slot has a length and a row of the page table, which names its pages in order; pages can be shared between
  * slots and are counted.  Everything is device memory of the caller; the calls read lengths and tables on the device, so that a
  * whole step can be captured in a HIP graph and replayed as sequences grow.  Values found there that make no sense (a page outside the
- * pool, a length beyond the table's row) are never used as addresses: what depends on them reads as NaN, or is not written.
+ * pool, a length beyond the table's row) are never used as addresses: what depends on them reads as NaN, or is not written.  Causal rows in
+ * front of a missing page are right.
  *
  * A block of 64 tokens x d channels of one head is 64*d bytes, in the order in which a wavefront's lanes take the operands of their matrix
  * instructions (every load of the attention kernel is 1 KB of neighbouring bytes, and nothing passes through LDS):

@@ -383,7 +383,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                     if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
                 }
             load_k(nblk);
-            rescale(masked(j) ? softmax(std::true_type{}, s, j * kBlock) : softmax(std::false_type{}, s, 0));
+            Factors f;
+            if (masked(j)) {
+                // no page: what was loaded in its place may be NaN, which the weights of zero of rows that do not see it would not take off
+                if (vs != vs) {
+#pragma unroll
+                    for (int i = 0; i < NL; ++i) vx[i] = make_uint4(0, 0, 0, 0);
+                }
+                f = softmax(std::true_type{}, s, j * kBlock);
+            } else {
+                f = softmax(std::false_type{}, s, 0);
+            }
+            rescale(f);
             // O^T += V^T P^T
 #pragma unroll
             for (int t = 0; t < OT; ++t) {
@@ -436,7 +447,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                 p[64 * (2 * (KN * wave + i) + 1)] = codes_to_half<E4M3>(kq[i].z, kq[i].w);
             }
         };
-        const auto convert_v = [&](int buf) {
+        const auto convert_v = [&](int buf, float scale) {
+            if (scale != scale) vq[0] = vq[1] = make_uint4(0, 0, 0, 0);  // (no page; as in the loop above)
             v8h *p = reinterpret_cast<v8h *>(stage + HALF * (2 + buf)) + 256 * wave + lane;
             p[0] = codes_to_half<E4M3>(vq[0].x, vq[1].x);
             p[64] = codes_to_half<E4M3>(vq[0].y, vq[1].y);
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                 __builtin_amdgcn_sched_barrier(0);
             }
             convert_k(BUF);
-            convert_v(BUF ^ 1);
+            convert_v(BUF ^ 1, vs1);
             ks = ks1, vs = vs1, ks1 = ks2, vs1 = vs2;
             next_block(j + 3);
             fetch_k(blk);
@@ -524,7 +536,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
         clear();
         if (jb < je_all) {
             convert_k(0);
-            convert_v(0);
+            convert_v(0, vs);
             next_block(jb + 1);
             fetch_k(blk);
             fetch_v(blk);

@@ -171,3 +171,22 @@ def test_blocks_of_v_very_far_apart_stay_finite(d, rows, loud):
     q = (torch.randn(rows, 8, d, generator=torch.Generator().manual_seed(rows)) * 2.0 ** -40).to(dt)
     out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=False, max_len=n)
     _bounded_by_own_blocks(out, q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), dt, f"{rows} rows", causal=False)
+
+
+@pytest.mark.parametrize("d,n,rows,Hq,block", [(64, 200, 12, 1, 3), (64, 300, 48, 1, 4), (64, 300, 60, 1, 4), (64, 300, 130, 2, 4), (128, 260, 10, 1, 4),
+                                              (128, 300, 60, 1, 4), (128, 300, 130, 1, 4), (128, 300, 130, 1, 3), (128, 300, 299, 1, 0)])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_rows_that_do_not_see_a_missing_page_stay_clean(d, n, rows, Hq, block, fmt):
+    """Causal rows in front of a block without a page, in one tile with rows that see it: whatever the pool's first page holds."""
+    dt = torch.float16
+    cache = make_cache([n], Hkv=1, d=d, dtype=dt, fmt=fmt, page_tokens=64, seed=0, spare=40)
+    table = cache.pages.table[0].tolist()
+    assert 0 not in table                                 # nobody's: NaN codes, where the format has them
+    q = torch.randn(rows, Hq, d, generator=torch.Generator().manual_seed(1)).to(dt)
+    want, err = attention(q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), causal=True)
+    cache.pages.table[0, block] = -1
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=True, max_len=n).double().cpu()
+    clean = max(0, 64 * block - (n - rows + 1) + 1)       # row i sees n - rows + i + 1 tokens
+    assert clean < rows and out[clean:].isnan().all()
+    tol = err + EPS[dt] * (want.abs() + err) + 2.0 ** -24
+    assert bool(((out - want).abs() <= tol)[:clean].all())
