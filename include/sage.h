@@ -429,6 +429,7 @@ typedef struct {
  *   SAGE_ROPE_NTK     with base * factor^(rot/(rot-2)) for the base
  *   SAGE_ROPE_YARN    f_i (1 - g) + f_i / factor * g, g rising from 0 to 1 over i between the pair that turns `high` times over
  *                     trained_len tokens (rounded down) and the one that turns `low` times (rounded up); magnitude 0.1 ln(factor) + 1 if 0 is given
+ *                     (factors below 1 bring that below 1: give 1 for none)
  *   SAGE_ROPE_BANDS   f_i g + f_i / factor * (1 - g), g = (turns over trained_len - low) / (high - low) within 0 .. 1
  * A plan holds f_i / (2 pi) in units of 2^-64 turns: position times frequency is then an exact product modulo one turn, so far
  * positions lose nothing.
@@ -470,7 +471,8 @@ int sage_rope(const void *q, void *q_out, const void *k, void *k_out, const int3
  * Append T tokens.  The slots' lengths and pages already cover them (sage_pages_reserve): the last of sequence b's rows becomes
  * token lens[slot] - 1.  Blocks that the tokens touch are written whole; the tokens that stood in a block begun before come
  * from the slot's tail, so codes and scales do not depend on how many calls brought the tokens.  A sequence may be shortened (lower
- * lens) to any length down to 64 tokens below the longest it has had, and goes on from there: drafted tokens are taken back so.  With
+ * lens) to any length down to 64 tokens below the longest that it, or the one it was forked from, has had, and goes on from there: drafted
+ * tokens are taken back so (until the next append the block that it ends in keeps the scale that they gave it, NaN if one was not finite).  With
  * `rope`, K is rotated by its index in the sequence, and rounded to `dt`, on the way.
  *   k, v       device, [T, Hkv, d] of cache->dt through strides {token, head} as for sage_rope         (in)
  * A slot may appear once in a call.
@@ -499,10 +501,11 @@ int sage_paged_gather(const sage_page_table *pages, const sage_cache *cache, voi
  *   q, out      device, [T, Hq, d] of cache->dt through strides {token, head} as for sage_rope; Hq a multiple of Hkv  (in, out)
  *   causal      1: the i-th of a sequence's n rows sees its first lens - n + i + 1 tokens (the rows are the last tokens of the
  *               sequence); 0: all rows see all tokens.  A row that sees none is zeros.
- *   max_len     the longest sequence the caller expects, 1 .. 2^22: sizes the launch.  Longer ones are right too, only slower.
+ *   max_len     the longest sequence the caller expects, 1 .. 2^22: sizes the launch.  Longer ones are right too, only slower; so is a
+ *               bound far above the sequences there are, which the library's choice of ranges goes by.
  *   split_keys  tokens per range: the keys of a sequence are cut into ranges that separate workgroups take, combined by a second
  *               launch; a positive multiple of 64, or 0 for the library's choice, which sage_paged_split_keys reports.  A row's result
- *               depends on its own sequence, T/B (which picks the row tile) and split_keys alone.
+ *               depends on its own sequence, T/B (which picks the row tile), split_keys and the number of ranges, max_len / split_keys, alone.
  *   workspace   device, 256-byte aligned, >= sage_paged_workspace_bytes() (0 bytes: none needed, may be NULL); nothing in
  *               it has to be initialised
  *   sm_scale    as for the other attention calls
@@ -531,8 +534,8 @@ int sage_attn_fwd_paged(const void *q, void *out, const int64_t *q_strides, cons
  *                     shortened sequence kept are used first.
  * sage_pages_fork     slot dst[i] becomes a copy of slot src[i]: full pages are shared, a last page that is not full gets a copy of its
  *                     own, which sage_pages_copy makes from page_moves[i] = {from, to} (-1, -1: none) and slot_moves[i] = {src, dst}
- *                     (the tails; -1, -1 for a refused entry) in each layer's cache.  Refused: slots outside the table, a dst that is not
- *                     empty, listed before or a src of this call, a pool without room.
+ *                     (the tails; -1, -1 for a refused entry) in each layer's cache.  Refused: slots outside the table, a src that is
+ *                     listed as a dst, a dst that has tokens or pages or is listed before, a pool without room.
  * sage_pages_free     the slots' pages are given back (freed when no slot names them) and the slots are empty.  Slots outside the table and
  *                     empty ones are passed over.
  * sage_pages_compact  the live pages behind the first M (M: the number of live ones) move to the lowest free places, at most max_moves

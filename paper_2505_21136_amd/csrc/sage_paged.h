@@ -80,7 +80,7 @@ __device__ __forceinline__ int page_of(const sage_page_table &pt, int slot, int 
 }
 
 // cos and sin of position * f: the product of the position and f / (2 pi) * 2^64 modulo 2^64 is the angle's fraction of a turn, exactly;
-// its upper 32 bits are kept (2^-33 turns off at most) and handed to the hardware's sine and cosine, which take turns.
+// its upper 32 bits are kept (less than 2^-32 turns off) and handed to the hardware's sine and cosine, which take turns.
 __device__ __forceinline__ void rope_angle(int pos, uint64_t f, float &c, float &s) {
     const uint32_t lo = (uint32_t)f, hi = (uint32_t)(f >> 32), p = (uint32_t)pos;
     uint32_t turn = __umulhi(lo, p) + hi * p;

@@ -1,5 +1,5 @@
 // The page table of a paged cache on the device (gfx950): reserving, forking, freeing and compacting.  Whole numbers only, bound by latency:
-// what has to be in order -- which free page goes to whom -- is one workgroup's scan of the reference counts, 32 a thread and round;
+// what has to be in order -- which free page goes to whom -- is one workgroup's scan of the reference counts, 4 or 16 a thread and round;
 // what has not, the tables' rows, is one workgroup per slot.
 #include "sage_paged.h"
 
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(const sage_page_table
             m += p < pt.n_pages && p >= live && r[e] > 0;
             f += p < live && r[e] <= 0;
         }
-        // (both sums in one scan: at most 2^15 of either in a round, and unsigned they fit)
+        // (both sums in one scan: at most 2^14 of either in a round)
         const int before = scan(m << 16 | f, total, shared);
         int km = movers + (int)((uint32_t)before >> 16), kf = holes + (before & 0xffff);
 #pragma unroll

@@ -122,7 +122,7 @@ def rope_plan(rot: int, *, base: float = 10000.0, layout: str = "half", scaling:
 def sage_rope(q: torch.Tensor, positions: torch.Tensor, plan: _RopePlan, *, k: torch.Tensor | None = None, transposed: bool = False,
               out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
     """Rotary positions of q [T, Hq, d] and, in the same launch, k [T, Hkv, d] (any views with contiguous channels): -> out, or (out, k_out).
-    out = q and k_out = k rotate in place."""
+    out = q and k_out = k rotate in place.  Autograd is not told: the gradient of out is turned back by a call with ``transposed``."""
     qs, (T, Hq, d), Hkv = _rows(q, "q"), q.shape, 0
     qos = ks = kos = None
     if out is None:

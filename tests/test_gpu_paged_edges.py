@@ -190,3 +190,16 @@ def test_rows_that_do_not_see_a_missing_page_stay_clean(d, n, rows, Hq, block, f
     assert clean < rows and out[clean:].isnan().all()
     tol = err + EPS[dt] * (want.abs() + err) + 2.0 ** -24
     assert bool(((out - want).abs() <= tol)[:clean].all())
+
+
+def test_a_chain_of_forks_in_one_call():
+    """A slot that a call fills cannot be copied by the same call: the entry with that source is refused, the one that fills it is not."""
+    pages, cache = empty(4, 1, 64, torch.float16, "int8", 64, 2)
+    sage.sage_pages_reserve(pages, ints(70, 64), ints(0, 3))
+    status, moves, slot_moves = sage.sage_pages_fork(pages, ints(0, 1, 3), ints(1, 2, 2))
+    assert status.tolist() == [0, -1, -1]                 # (the last one's destination is listed before)
+    assert slot_moves.tolist() == [[0, 1], [-1, -1], [-1, -1]] and moves[1:].tolist() == [[-1, -1], [-1, -1]]
+    assert pages.lens.tolist() == [70, 70, 0, 64] and pages.table[2].tolist() == [-1, -1]
+    # a slot that is not empty is not filled, and its name as a destination still bars it as a source
+    status, _, _ = sage.sage_pages_fork(pages, ints(0, 1), ints(1, 2))
+    assert status.tolist() == [-1, -1]
