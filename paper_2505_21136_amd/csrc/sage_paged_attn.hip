@@ -296,10 +296,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
             for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < R; ++i) top = fmaxf(top, s[n_][t][i]);
-            const float m_new = fmaxf(m[n_], Mfma<M>::row_max(top) * c);
+            top = Mfma<M>::row_max(top);
+            const float m_new = fmaxf(m[n_], top * c);
             const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
             const float alpha = __builtin_amdgcn_exp2f(m[n_] - base);
-            const float shift = (e < 128 ? lr : __builtin_nanf("")) - base;
+            float shift = (e < 128 ? lr : __builtin_nanf("")) - base;
+            // (scores beyond 2^23: the rounding of the maximum and of this sum can lift the largest weight out of binary16's range)
+            const float most = __builtin_fmaf(top, c, shift);
+            shift -= most > kLift + 1.5f ? most : 0.0f;
             float sum = 0.0f;
 #pragma unroll
             for (int st = 0; st < NP / 8; ++st) {

@@ -173,6 +173,28 @@ def test_blocks_of_v_very_far_apart_stay_finite(d, rows, loud):
     _bounded_by_own_blocks(out, q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), dt, f"{rows} rows", causal=False)
 
 
+@pytest.mark.parametrize("exponent", [8, 16, 22, 23, 24, 25, 26, 27])
+@pytest.mark.parametrize("d,rows,fmt", [(64, 1, "int8"), (64, 12, "e4m3"), (64, 40, "int8"), (128, 1, "e4m3"), (128, 8, "int8"), (128, 40, "e4m3")])
+def test_scores_of_all_sizes_that_one_key_wins(exponent, d, rows, fmt):
+    """Scores up to 2^exponent, in powers of two: where the largest is ahead by more than what binary32 sums of d products leave open, and 40 more,
+    the row is that key's V: P~'s and the output's rounding off, and what n others can weigh."""
+    n, dt = 300, torch.bfloat16
+    cache = make_cache([n], Hkv=2, d=d, dtype=dt, fmt=fmt, page_tokens=64, seed=d + rows)
+    q = torch.randn(rows, 8, d, generator=torch.Generator().manual_seed(3)).to(dt)
+    k, v = sequence(cache, "k", 0, n), sequence(cache, "v", 0, n)
+    raw = torch.stack([q[:, h].double() @ k[:, h // 4].T for h in range(8)], 1)
+    sm = 2.0 ** exponent * math.log(2) / float(raw.abs().max())
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=False, max_len=n, sm_scale=sm).double().cpu()
+    two = (raw * sm).topk(2, -1)
+    big = torch.stack([q[:, h].double().abs() @ k[:, h // 4].abs().T for h in range(8)], 1).amax(-1) * sm
+    sure = two.values[..., 0] - two.values[..., 1] > 40 + 2 * (d + 8) * 2.0 ** -24 * big
+    assert bool(sure.any()) and bool(out.isfinite().all())
+    at = two.indices[..., 0]
+    want = torch.stack([v[at[:, h], h // 4] for h in range(8)], 1)
+    tol = want.abs() * (2.0 ** -11 + 2.0 ** -19 + EPS[dt]) * (1 + 2.0 ** -8) + n * math.exp(-40) * float(v.abs().max())
+    assert bool(((out - want).abs() <= tol)[sure].all())
+
+
 @pytest.mark.parametrize("d,n,rows,Hq,block", [(64, 200, 12, 1, 3), (64, 300, 48, 1, 4), (64, 300, 60, 1, 4), (64, 300, 130, 2, 4), (128, 260, 10, 1, 4),
                                               (128, 300, 60, 1, 4), (128, 300, 130, 1, 4), (128, 300, 130, 1, 3), (128, 300, 299, 1, 0)])
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
