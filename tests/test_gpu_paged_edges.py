@@ -225,3 +225,55 @@ def test_a_chain_of_forks_in_one_call():
     # a slot that is not empty is not filled, and its name as a destination still bars it as a source
     status, _, _ = sage.sage_pages_fork(pages, ints(0, 1), ints(1, 2))
     assert status.tolist() == [-1, -1]
+
+
+# ---- sizes at which the kernels change their ways -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("ranges", [17, 20, 32, 33, 257, 300])
+@pytest.mark.parametrize("d,rows", [(64, 1), (128, 3)])
+def test_many_ranges(ranges, d, rows):
+    # up to 32 ranges are combined by each thread, more by the row's threads together, 256 at a time
+    run_case([64 * ranges - 5, 64, 130], [rows, 1, 1], Hq=2, Hkv=1, d=d, dtype="bf16", fmt="int8", page=256, causal=True, seed=ranges, split=64)
+
+
+@pytest.mark.parametrize("n_pages,n", [(3000, 1500), (9000, 4096), (40000, 4096)])
+def test_lists_and_tables_of_the_largest_size(n_pages, n):
+    g = torch.Generator().manual_seed(n)
+    slots, width = 4096, 12
+    pages = sage.PageTable.empty(n_pages, page_tokens=64, slots=slots, width=width, device=DEV)
+    sim = Table(pages)
+    perm = lambda k: torch.randperm(slots, generator=g)[:k].tolist()  # noqa: E731
+    s, m = perm(slots // 2), torch.randint(0, 200, (slots // 2,), generator=g).tolist()
+    assert sage.sage_pages_reserve(pages, ints(*m), ints(*s)).tolist() == sim.reserve(s, m)
+    sim.same(pages)
+    # sources with and without tokens, destinations of which some are in use or listed twice
+    src, dst = torch.randint(0, slots, (n,), generator=g).tolist(), perm(n) if n < slots else torch.randint(0, slots, (n,), generator=g).tolist()
+    dst = [-1 if i % 3 else t for i, t in enumerate(dst)] if n == slots else dst
+    status, pm, sm = sage.sage_pages_fork(pages, ints(*src), ints(*dst))
+    want = sim.fork(src, dst)
+    assert (status.tolist(), pm.tolist(), sm.tolist()) == want and 0 in want[0] and -1 in want[0]
+    sim.same(pages)
+    s, m = perm(n) if n < slots else perm(slots), torch.randint(0, 300, (n,), generator=g).tolist()
+    assert sage.sage_pages_reserve(pages, ints(*m), ints(*s)).tolist() == sim.reserve(s, m)
+    sim.same(pages)
+    assert sage.sage_pages_reserve(pages).tolist() == sim.reserve(list(range(slots)), [1] * slots)
+    gone = perm(slots)[:3000]
+    sage.sage_pages_free(pages, ints(*gone))
+    sim.free(gone)
+    moves, counts = sage.sage_pages_compact(pages, n_pages // 2)
+    assert (moves.tolist(), counts.tolist()) == sim.compact(n_pages // 2)
+    sim.same(pages)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("scaling,magnitude", [("yarn", 0.0), ("none", 0.5)])
+def test_an_append_with_a_magnitude(layout, scaling, magnitude):
+    d, Hkv, dt, n = 128, 2, torch.bfloat16, 150
+    pages, cache = empty(1, Hkv, d, dt, "int8", 128, 2)
+    plan = sage.rope_plan(96, layout=layout, scaling=scaling, factor=8.0, trained_len=64, magnitude=magnitude)
+    assert plan.magnitude != 1.0
+    k, v = (torch.randn(n, Hkv, d, device=DEV).to(dt) for _ in "kv")
+    for a, b in ((0, 70), (70, 71), (71, n)):
+        sage.sage_pages_reserve(pages, ints(b - a))
+        sage.sage_paged_append(cache, k[a:b], v[a:b], rope=plan)
+    check_blocks(cache, 0, {"k": sage.sage_rope(k, torch.arange(n, dtype=torch.int32, device=DEV), plan).cpu(), "v": v.cpu()})
