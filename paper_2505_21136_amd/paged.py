@@ -82,6 +82,14 @@ def _ours(pages: "PageTable") -> None:
         raise _sage.SageError(f"the page table is on device {pages.device_index}, the current device is {_current()}")
 
 
+def _room(t: torch.Tensor) -> int:
+    """The bytes of a caller's workspace."""
+    if not t.is_contiguous():
+        raise _sage.SageError("workspace must be contiguous: its bytes are counted from its first one on")
+    _here(t, "workspace")
+    return t.numel() * t.element_size()
+
+
 def _ints(t: torch.Tensor | None, what: str, n: int | None = None) -> int | None:
     """The address of a contiguous int32 list (of n entries)."""
     if t is None:
@@ -300,12 +308,10 @@ def sage_attn_fwd_paged(q: torch.Tensor, cache: PagedCache, *, causal: bool, max
     B = _batch(cache, q_start, slots, "q_start")
     if workspace is None:
         workspace = _sage._workspace(paged_workspace_bytes(T, B, Hq, cache.Hkv, d, max_len, split_keys), q.device)
-    else:
-        _here(workspace, "workspace")
+    room = _room(workspace)
     _sage._check(_sage.lib().sage_attn_fwd_paged(
         q.data_ptr(), out.data_ptr(), qs, os_, cache.pages.ref, cache.ref, _ints(q_start, "q_start"), _ints(slots, "slots", B), B, T, Hq,
-        int(max_len), int(causal), float(sm_scale), int(split_keys), _sage._stream(), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size()))
+        int(max_len), int(causal), float(sm_scale), int(split_keys), _sage._stream(), workspace.data_ptr(), room))
     return out
 
 
@@ -342,12 +348,10 @@ def sage_pages_compact(pages: PageTable, max_moves: int | None = None, *, worksp
     copies in each layer's cache."""
     most = max(1, pages.n_pages // 2) if max_moves is None else int(max_moves)
     _ours(pages)
-    if workspace is not None:
-        _here(workspace, "workspace")
     moves, counts = pages.refs.new_empty((max(most, 0), 2)), pages.refs.new_empty(2)
     ws = workspace if workspace is not None else pages.refs.new_empty((pages.n_pages + 63) // 64 * 64)
-    _sage._check(_sage.lib().sage_pages_compact(pages.ref, moves.data_ptr(), most, counts.data_ptr(), _sage._stream(), ws.data_ptr(),
-                                                ws.numel() * ws.element_size()))
+    room = _room(ws)
+    _sage._check(_sage.lib().sage_pages_compact(pages.ref, moves.data_ptr(), most, counts.data_ptr(), _sage._stream(), ws.data_ptr(), room))
     return moves, counts
 
 

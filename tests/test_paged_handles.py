@@ -53,3 +53,15 @@ def test_values_are_changed_in_place(handles):
     cache.v_scale.mul_(2.0)
     cache.v_scale *= 2.0
     assert pages.lens.tolist() == [8, 6, 7] and pages.lens.data_ptr() == at == pages._c.lens
+
+
+def test_a_workspace_of_fewer_bytes_than_elements_is_refused(handles):
+    """A broadcast tensor has as many elements as one likes and the memory of one: the calls would write behind it."""
+    pages, cache = handles
+    q = torch.zeros(3, 2, 64, dtype=torch.float16)
+    wide = torch.zeros(64, dtype=torch.uint8).expand(1 << 16, 64)
+    for ws in (wide, wide.flatten()[:1].expand(1 << 20), torch.zeros(1 << 16)[::2]):
+        for call in (lambda: sage.sage_attn_fwd_paged(q, cache, causal=True, max_len=128, split_keys=64, workspace=ws),
+                     lambda: sage.sage_pages_compact(pages, workspace=ws)):
+            with pytest.raises(sage.SageError, match="workspace must be contiguous"):
+                call()
