@@ -30,11 +30,11 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = SAGE_CACHE_BLOCK, kAttnWaves = 4;
-// O stands in units of 2^(ref - kLift), where 2^ref is near the V scales of late; a block's scale over that unit goes into P~.  ref moves to a block's
-// own power of two where that is larger or kNear below: O is then multiplied by a power of two, exactly.  A weight p of a row (its largest
-// is 1) becomes p * 2^(kLift - kNear) .. p * 2^(kLift + 1), which binary16 holds with all its bits down to p = 2^-20 and not at all
-// only below 2^-31, whatever the scales of the blocks before.  It never falls more than kSpan below the largest so far, so that O stays finite: keys
-// whose V is 2^-kSpan of others' lose precision.
+// O stands in units of 2^ref, and a block's V scale over that unit goes into P~.  The unit is 2^-kLift of a power of two e near the V scales of
+// late, which moves to a block's own where that is above, or more than kNear below: O is then multiplied by a power of two, exactly.  A weight p of a
+// row (its largest is 1) becomes p * 2^(kLift - kNear) .. p * 2^(kLift + 1), which binary16 holds with all its bits down to p = 2^-20 and not
+// at all only below 2^-31, whatever the scales of the blocks before.  e never falls more than kSpan below the largest so far, so that O stays
+// finite: keys whose V is 2^-kSpan of others' lose precision.
 constexpr int kLift = 14, kNear = 8, kSpan = 60, kNoRef = -512;
 
 struct PagedArgs {
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
         for (int n_ = 0; n_ < NT; ++n_) convert_rows(qx[n_], qh[n_], row_scale[n_]);
     };
     float m[NT], l[NT];
-    int vexp = kNoRef, vtop = kNoRef;  // ref, and the largest that it would have been
+    float ref = kNoRef, top_e = kNoRef;  // the logarithm of o's unit, and of the largest V scale's power of two so far
     acc_t o[NT][OT];
 #pragma unroll
     for (int n_ = 0; n_ < NT; ++n_) m[n_] = -INFINITY, l[n_] = 0.0f;
@@ -265,22 +265,35 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
     struct Factors {
         float of[NT];
     };
-    // The softmax of one block's scores: P~ as the operand of P V, times the block's V scale over o's unit; returns what o is to be
-    // multiplied by.  MASKED: some row does not see some key of the block.
-    const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0) {
+    // What the block's V scale does to the weights and to o: it is multiplied into the weights as an exponent, lr; `unlift` takes it out of their
+    // sum; `back` is what o changes its unit by.  Most blocks need no other unit: one comparison.  A block of zeros: any exponent will do.
+    struct Lift {
+        float lr, unlift, back;
+    };
+    const auto lift = [&]() {
+        const float v2 = __builtin_amdgcn_logf(vs);
+        Lift w{v2 - ref, 0.0f, 1.0f};
+        w.unlift = __builtin_amdgcn_exp2f(-w.lr);
+        if (!(w.lr >= kLift - kNear && w.lr < kLift + 1)) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, vs);
+            w.lr = bits == 0 ? 0.0f : __builtin_nanf(""), w.unlift = 1.0f;
+            if (bits - 1 < 0x7f7fffffu) {
+                const float e = (float)((int)(bits >> 23) - 127);
+                top_e = fmaxf(top_e, e);
+                const float to = fmaxf(e, top_e - kSpan) - kLift;
+                w.back = __builtin_amdgcn_ldexpf(1.0f, (int)(ref - to));
+                ref = to;
+                w.lr = fmaxf(v2 - ref, kLift - kSpan);
+                w.unlift = __builtin_amdgcn_exp2f(-w.lr);
+            }
+        }
+        return w;
+    };
+    // The softmax of one block's scores: P~ as the operand of P V; returns what o is to be multiplied by.  MASKED: some row does not
+    // see some key of the block.
+    const auto softmax = [&](auto masked_c, acc_t (&s)[NT][KT], int key0, const Lift &w) {
         constexpr bool MASKED = decltype(masked_c)::value;
         Factors f;
-        // V's scale goes into the exponent: its power of two over the unit, and the logarithm of what is left, 1 .. 2 (a block of zeros: any will do)
-        const uint32_t vbits = __builtin_bit_cast(uint32_t, vs);
-        const int e = (int)(vbits >> 23) - 127;  // (128: not finite)
-        const bool counts = vs > 0.0f && e < 128;
-        vtop = counts ? max(vtop, e) : vtop;
-        const int ref = counts && (e > vexp || e < vexp - kNear) ? max(e, vtop - kSpan) : vexp, moved = vexp - ref;
-        const float back = moved < -126 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(127 + moved) << 23);
-        const float rest = __builtin_amdgcn_logf(__builtin_bit_cast(float, (vbits & 0x7fffffu) | 0x3f800000u));
-        const float lr = counts ? (float)max(e - ref, -kSpan) + (rest + kLift) : 0.0f;
-        const float unlift = __builtin_amdgcn_exp2f(-lr);
-        vexp = ref;
 #pragma unroll
         for (int n_ = 0; n_ < NT; ++n_) {
             const auto hidden = [&](int t, int i) { return key0 + M * t + 8 * (i >> 2) + 4 * g + (i & 3) > lim[n_]; };
@@ -300,7 +313,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
             const float m_new = fmaxf(m[n_], top * c);
             const float base = m_new == -INFINITY ? 0.0f : m_new;  // (a row that has seen nothing: every weight is 2^-inf)
             const float alpha = __builtin_amdgcn_exp2f(m[n_] - base);
-            float shift = (e < 128 ? lr : __builtin_nanf("")) - base;
+            float shift = w.lr - base;
             // (scores beyond 2^23: the rounding of the maximum and of this sum can lift the largest weight out of binary16's range)
             const float most = __builtin_fmaf(top, c, shift);
             shift -= most > kLift + 1.5f ? most : 0.0f;
@@ -315,12 +328,12 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                     if constexpr (MASKED) p[e] = hidden(t, i) ? 0.0f : p[e];  // (and no NaN of the scales comes in)
                     sum += p[e];
                 }
-                const uint4 w = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
-                pb[n_][st] = __builtin_bit_cast(v8h, w);
+                const uint4 packed = make_uint4(pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7]));
+                pb[n_][st] = __builtin_bit_cast(v8h, packed);
             }
-            l[n_] = l[n_] * alpha + sum * unlift;
+            l[n_] = l[n_] * alpha + sum * w.unlift;
             m[n_] = m_new;
-            f.of[n_] = alpha * back;
+            f.of[n_] = alpha * w.back;
         }
         return f;
     };
@@ -387,6 +400,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
                     if constexpr (M == 32) __builtin_amdgcn_sched_barrier(0);
                 }
             load_k(nblk);
+            const Lift w = lift();
             Factors f;
             if (masked(j)) {
                 // no page: what was loaded in its place may be NaN, which the weights of zero of rows that do not see it would not take off
@@ -394,9 +408,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
 #pragma unroll
                     for (int i = 0; i < NL; ++i) vx[i] = make_uint4(0, 0, 0, 0);
                 }
-                f = softmax(std::true_type{}, s, j * kBlock);
+                f = softmax(std::true_type{}, s, j * kBlock, w);
             } else {
-                f = softmax(std::false_type{}, s, 0);
+                f = softmax(std::false_type{}, s, 0, w);
             }
             rescale(f);
             // O^T += V^T P^T
@@ -489,12 +503,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
         const auto step = [&](int j, acc_t (&now)[NT][KT], acc_t (&then)[NT][KT], auto buf_c) {
             constexpr int BUF = decltype(buf_c)::value;
             if (j < je) {
+                const Lift w = lift();
                 Factors f;
                 const auto both = [&](auto masked_c) {
                     __builtin_amdgcn_s_setprio(1);
                     __builtin_amdgcn_sched_barrier(0);
                     scores(then, BUF ^ 1);
-                    f = softmax(masked_c, now, j * kBlock);
+                    f = softmax(masked_c, now, j * kBlock, w);
                     // a matrix instruction, an operand four ahead, and what the vector unit does meanwhile
                     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -570,7 +585,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
 
     // ---- the key groups' sums ----
     const PagedArgs z = arguments_again();
-    const float unit = vexp < -112 ? 0.0f : __builtin_bit_cast(float, (uint32_t)(127 + vexp - kLift) << 23);  // (below: nothing but zeros was seen)
+    const float unit = __builtin_amdgcn_ldexpf(1.0f, (int)ref);
     const auto sums_at = [&](int n_, int t, int i) {
         return make_float4(o[n_][t][i] * unit, o[n_][t][i + 1] * unit, o[n_][t][i + 2] * unit, o[n_][t][i + 3] * unit);
     };
