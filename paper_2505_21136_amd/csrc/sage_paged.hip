@@ -58,8 +58,8 @@ struct AppendArgs {
 //   V: a thread takes 2 channels of the 16 tokens whose codes are neighbours in the cache, 16 bytes per channel; a wavefront's loads are
 //      whole rows of 256 bytes.
 // Bound by memory where there is much of it (one prompt of 32768 tokens x 8 heads x 128: 39 us = 5.2 TB/s; 64 sequences' one token each, 8 KB of tail
-// read and 8 KB of codes written per head: 10 us, 512 36 us), by the chain length -- tokens -- maximum -- codes where there is little (one
-// sequence 5.4 us; ten ragged prompts of 12600 tokens, rotated, 27 us).
+// read and 8 KB of codes written per head: 10 us, 512 37 us), by the chain length -- tokens -- maximum -- codes where there is little (one
+// sequence 5.8 us; ten ragged prompts of 12600 tokens, rotated, 27 us).
 // Values stay in registers in 16 bits and are widened twice, for the maximum and for the codes: 80 registers, six wavefronts per SIMD, which
 // the chain table -- tokens -- maximum -- codes needs to keep memory busy.
 // The tail's two halves hold the tokens of the sequence's last two blocks.  The half that the first touched block stands in is

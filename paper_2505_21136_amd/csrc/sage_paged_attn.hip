@@ -13,7 +13,7 @@
 //
 // What bounds it.  Up to 16 rows per K/V head: memory; 64 sequences x 16384 tokens, 32 heads over 8, d 128: 360 us = 6.0 TB/s, 95 % of what a read
 // reaches; 48 of 1000 to 8192 tokens 96 us = 4.8 TB/s, of which the combination is 5 and the ends of a launch of unequal sequences most of
-// the rest.  A few sequences: the chain of two launches and what one CU reads, about 70 GB/s (2 x 1500 tokens 9.8 us; in one range, on 16 CUs,
+// the rest.  A few sequences: the chain of two launches and what one CU reads, about 70 GB/s (2 x 1500 tokens 9.9 us; in one range, on 16 CUs,
 // 11.9, and the same with eight wavefronts in a workgroup).  32 rows and more: vector issue; see below.  Page ids and scales come
 // through the scalar cache: as vector loads they were waited for in order, behind everything fetched ahead (16 rows, 256 sequences x 1000
 // tokens 68 -> 62 us; 8 heads x 32768 in one range 188 -> 161).
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, M * NT == 16 ? 3 : 2) void paged_r
         // instructions, with the wavefront's priority raised; P V follows, with its operands four ahead.  A barrier per block.
         // Measured, 4 sequences x 1024 rows x 4096 tokens, 32 heads over 8, not causal (a library's 16-bit product would take 225 us at its
         // rate), INT8 / E4M3: each wavefront on its own 348 / 318 us, conversions shared 328 / 318, scores under the exponentials and operands
-        // ahead 315 / 304, priority raised 302 / 294; matrix pipe 37 % and vector issue 48 % of the time, and little of the two overlaps.  At
+        // ahead 315 / 304, priority raised 302 / 294; matrix pipe 41 % and vector issue 52 % of the time, and little of the two overlaps.  At
         // d = 64, half the conversions, none of this is faster than a wavefront on its own (211 us; 208 to 215).
         uint4 qx[NT][QS];
         load_q(qx);
@@ -750,7 +750,7 @@ int paged_auto_split_keys(int T, int B, int Hq, int Hkv, int max_len) {
     const int64_t blocks = cdiv(max_len, kBlock);
     // Fewer workgroups than CUs: ranges for one workgroup per CU, of four blocks at least -- more of them cost more in the combination than
     // their wavefronts hide -- and none up to twelve blocks, where the second launch costs more than it saves (32 heads over 8, one sequence, us: 768
-    // tokens 8.5 in one range and 8.9 in three at d 128, 7.0 and 8.0 at d 64; 1280 tokens 10.6 and 9.7, 8.7 and 8.7).
+    // tokens 8.8 in one range and 9.2 in three at d 128, 7.1 and 8.2 at d 64; 1280 tokens 11.0 and 9.9, 8.9 and 8.9).
     // Ranges of 32 blocks and more cost little, so there are more of them where sequences of different lengths would leave CUs idle: up to two
     // per CU (16 rows, 24 sequences of 2000 to 16384 tokens, 8 heads, d 64: one range 67, two 51, all of 16384 tokens 75 and 78; 32 rows, d 64, 16
     // sequences of 500 to 8192: one per CU 43, two 37; six of up to 512 rows over up to 16384 tokens, d 128: one range 454, two 284, four
