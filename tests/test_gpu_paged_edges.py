@@ -173,6 +173,24 @@ def test_blocks_of_v_very_far_apart_stay_finite(d, rows, loud):
     _bounded_by_own_blocks(out, q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), dt, f"{rows} rows", causal=False)
 
 
+@pytest.mark.parametrize("d,rows", ROWS)
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("zeros", [[0], [0, 1, 2, 3, 4], [9, 17], list(range(0, 18, 2)), list(range(18))])
+def test_blocks_of_zeros_among_others(d, rows, fmt, zeros):
+    # V's scale is 0 there, and K's in some: their keys have weight like others
+    n, dt = 64 * 18 - 9, torch.float16
+    cache = make_cache([n], Hkv=2, d=d, dtype=dt, fmt=fmt, page_tokens=64, seed=rows)
+    for j in zeros:
+        p = int(cache.pages.table[0, j])
+        cache.v[p], cache.v_scale[p] = 128 if fmt == "int8" else 0, 0.0
+        if j % 4 == 0:
+            cache.k[p], cache.k_scale[p] = 128 if fmt == "int8" else 0, 0.0
+    q = torch.randn(rows, 8, d, generator=torch.Generator().manual_seed(rows)).to(dt)
+    out = sage.sage_attn_fwd_paged(q.to(DEV), cache, causal=True, max_len=n)
+    _bounded_by_own_blocks(out, q, sequence(cache, "k", 0, n), sequence(cache, "v", 0, n), dt, f"{rows} rows")
+    assert len(zeros) < 18 or bool((out == 0).all())
+
+
 @pytest.mark.parametrize("exponent", [8, 16, 22, 23, 24, 25, 26, 27])
 @pytest.mark.parametrize("d,rows,fmt", [(64, 1, "int8"), (64, 12, "e4m3"), (64, 40, "int8"), (128, 1, "e4m3"), (128, 8, "int8"), (128, 40, "e4m3")])
 def test_scores_of_all_sizes_that_one_key_wins(exponent, d, rows, fmt):
