@@ -188,7 +188,7 @@ __device__ __forceinline__ void append_blocks(const AppendArgs &a, const sage_ro
         block_scale<E4M3>(amax, odd != 0.0f, scale, factor);
 
         // ---- codes and scale ----
-        if (page >= 0 && shares <= 1) {  // (a page of others too is theirs as well)
+        if (page >= 0 && shares <= 1) {  // (a page that other slots name too stays as it is)
             const size_t blk = ((size_t)page * Hkv + h) * per_page + in_page;
             uint8_t *out = (is_v ? a.c.v : a.c.k) + blk * (kBlock * D);
             if (tid == 0) (is_v ? a.c.v_scale : a.c.k_scale)[blk] = scale;
